@@ -22,6 +22,11 @@
  *   sd_sample_tokens     drafts drawn from their distributions,
  *                        T' ~ Categorical(P') (Algorithm 1)
  *
+ * Around the target's cache:
+ *
+ *   sd_rope              rotary positions of text, images and video
+ *   sd_kv_append         new rows rotated and written into the cache
+ *
  * Conventions shared by every entry point
  * ---------------------------------------
  * - Every tensor pointer is DEVICE memory on the current HIP device, owned by
@@ -39,7 +44,8 @@
  *   they read so that a violated precondition yields an unspecified result,
  *   never an out-of-bounds access.
  * - dtype: SD_F32 (float32 storage) or SD_BF16 (bfloat16 storage).  All
- *   arithmetic accumulates in float32 and all floating outputs are float32.
+ *   arithmetic accumulates in float32 and floating outputs are float32, unless
+ *   a call states another type.
  * - Workspace: a caller-owned device buffer of at least the size returned by
  *   the matching *_workspace_size function for the same shape arguments
  *   (NULL is allowed when that size is 0).  Two calls in flight at the
@@ -76,6 +82,12 @@ typedef enum sd_accept_mode {
   SD_ACCEPT_GREEDY = 0,     /* temperature 0: longest prefix equal to the target argmax */
   SD_ACCEPT_SAMPLED = 1     /* min(1, p/q) acceptance and residual resampling */
 } sd_accept_mode;
+
+/* frequencies of rotary pairs (sd_rope, sd_kv_append) */
+typedef enum sd_rope_freq {
+  SD_ROPE_RUNNING = 0,      /* theta^(-i / P), i counted over all axes */
+  SD_ROPE_PER_AXIS = 1      /* theta^(-i / n), i counted within the axis of n pairs */
+} sd_rope_freq;
 
 /* Human-readable name of a status code (static storage, never NULL). */
 const char* sd_status_string(int status);
@@ -527,6 +539,83 @@ int sd_semi_ar_draft(const void* u0, const void* fc_w, const float* fc_b, const 
                      int num_kv_heads, int I, int Lmax, int V, int K, int k_prime, float eps,
                      float theta, float temperature, void* workspace, size_t workspace_bytes,
                      void* stream);
+
+/* ------------------------------------------------------------------------
+ * Rotary positions with one to four axes: the text's one position, the
+ * height and width of image patches, the time, height and width of video
+ * tokens.  Of every head's D channels the first 2P form P pairs (i, i + P);
+ * axis a owns the next sections[a] of them (P = their sum), and with pair i
+ * of axis a (its first pair i0)
+ *
+ *   ang = pos[a, t] * theta^(-i / P)                     SD_ROPE_RUNNING
+ *   ang = pos[a, t] * theta^(-(i - i0) / sections[a])    SD_ROPE_PER_AXIS
+ *   y[t, h, i]     = x[t, h, i] cos(ang) - x[t, h, i + P] sin(ang)
+ *   y[t, h, i + P] = x[t, h, i] sin(ang) + x[t, h, i + P] cos(ang)
+ *
+ * the other D - 2P channels are copied.  With `inverse` non-zero the pairs
+ * turn by -ang: that undoes the rotation and is its gradient (the rotation is
+ * orthogonal, so that dx is dy turned back).
+ *
+ *   x, y      [T, H, D] dtype, rows of H D elements every x_stride / y_stride
+ *             elements; y may be x with the same stride (in place), else no
+ *             element of y is an element of x
+ *   pos       [num_axes, T] int32, any values
+ *   sections  [num_axes] HOST array, or NULL for one axis of D / 2 pairs
+ * Angles are reduced in float64, products are float32, y is rounded once to
+ * dtype (the one output here that is not float32: it feeds the attention).
+ * Requirements: T >= 0 (0 launches nothing), H >= 1, 1 <= num_axes <= 4,
+ * sections >= 1 with a sum of at most D / 2, D <= 256, T <= 2^30, H <= 2^20,
+ * strides >= H D and <= 2^32, theta > 0 and finite.  Any alignment that dtype
+ * allows; 16-byte rows and sections of whole 8s are the fast ones.  No
+ * workspace.  Errors: SD_ERR_INVALID_ARG, SD_ERR_UNSUPPORTED (num_axes, D, T
+ * or H beyond the limits).
+ * ---------------------------------------------------------------------- */
+int sd_rope(const void* x, int64_t x_stride, const int32_t* pos, void* y, int64_t y_stride,
+            int T, int H, int D, int num_axes, const int32_t* sections, float theta, int freq,
+            int inverse, int dtype, void* stream);
+
+/* ------------------------------------------------------------------------
+ * New rows of a layer into the cache that sd_verify_attention and
+ * sd_verify_shared read: keys are rotated and written with their values, the
+ * queries of the same rows are rotated beside them, in one launch.
+ *
+ * Row t belongs to sequence b where row_start[b] <= t < row_start[b + 1]
+ * (row_start NULL: T / B rows each).  The n_b rows of a sequence are its last
+ * cache entries: row row_start[b] + j takes cache position kv_len[b] - n_b +
+ * j, so that the kv_len given to the attention afterwards is this one.
+ *
+ *   q         [T, Hq, D] src_dtype, rows every q_stride elements (Hq = 0 and
+ *             NULL: keys and values only)
+ *   k, v      [T, Hkv, D] src_dtype, rows every k_stride / v_stride elements
+ *             (the three may be views of one fused projection)
+ *   q_out     [T, Hq, D] dtype, dense: the rotated queries.  May be q itself
+ *             where that is dense and of dtype; else apart from q, k and v
+ *   k_cache, v_cache  contiguous (page_table == NULL) [B, Lmax, Hkv, D] dtype,
+ *             or page pools [num_pages, Hkv, 16, D], apart from the rows read
+ *   row_start [B + 1] int32, not decreasing, or NULL (then B divides T).  Rows
+ *             before row_start[0] and from row_start[B] on are left out: their
+ *             q_out keeps what it held
+ *   kv_len    [B] int32: cache length after the append
+ *   page_table [B, max_pages] int32, or NULL
+ *   pos       [num_axes, T] int32 rotary positions, or NULL: the cache
+ *             position on every axis
+ *   num_axes, sections, theta, freq  as for sd_rope; num_axes = 0 turns
+ *             nothing (keys that carry their positions already)
+ * A row whose cache position lies outside 0 .. capacity - 1, or whose page id
+ * lies outside 0 .. num_pages - 1, is not written to the cache (its q_out is).
+ * Two rows never share a cache place unless page_table names a page twice;
+ * such a place gets one of the two rows.
+ * Requirements: T >= 0 (0 launches nothing), B, Hkv >= 1, Hq >= 0, D <= 256,
+ * T <= 2^30, Hq and Hkv <= 2^20, max_pages <= 2^26; src_dtype and dtype equal,
+ * or SD_F32 into SD_BF16 (SD_BF16 into SD_F32: SD_ERR_UNSUPPORTED).
+ * Rounding, alignment and errors as for sd_rope.
+ * ---------------------------------------------------------------------- */
+int sd_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                 const void* v, int64_t v_stride, void* q_out, void* k_cache, void* v_cache,
+                 const int32_t* row_start, const int32_t* kv_len, const int32_t* page_table,
+                 int max_pages, int num_pages, int Lmax, const int32_t* pos, int T, int B,
+                 int Hq, int Hkv, int D, int num_axes, const int32_t* sections, float theta,
+                 int freq, int src_dtype, int dtype, void* stream);
 
 #ifdef __cplusplus
 }

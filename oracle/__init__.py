@@ -29,6 +29,9 @@ reader can check it against the paper by eye:
   decoder layer whose placeholder rows give the next K draft states
   (Sec. 3.1, Sec. 3.3, Algorithm 1, Sec. 4.3); ``semi_ar_draft`` runs K
   drafts in K / k' passes of k' (the group size of the paper's ablation).
+* ``rope_axes`` / ``kv_append`` -- rotary positions with several axes, and new
+  rows rotated and written into the target's cache (pins in
+  ``tests/test_oracle_cache.py``).
 
 Readings of points the paper leaves open are stated in each module.  No
 function here is "parity unpinned": every one is checked in
@@ -42,6 +45,7 @@ from .lm_head import lm_head_logits, softmax_temperature, lm_head_probs, sample_
 from .accept_logits import philox4x64, philox_uniforms, spec_accept_logits
 from .draft_layer import (rms_norm, rope, linear, silu, swiglu, semi_ar_layer, semi_ar_draft, bf16_round,
                           dequantize_rows, linear_q8, semi_ar_layer_q8)
+from .rope import rope_angles, rope_axes, append_places, kv_append
 from .accept import (
     spec_accept,
     spec_accept_one,
@@ -90,4 +94,8 @@ __all__ = [
     "dequantize_rows",
     "linear_q8",
     "semi_ar_layer_q8",
+    "rope_angles",
+    "rope_axes",
+    "append_places",
+    "kv_append",
 ]

@@ -11,6 +11,8 @@ library is missing or the tensors are not on the GPU, the calls raise.
     sd_spec_accept       Sec. 3.1 / 3.3 acceptance; greedy for Sec. 4.2
     sd_lm_head_probs     Sec. 3.1 / 3.3, Algorithm 1: LM head + softmax(z / tau)
     sd_sample_tokens     Algorithm 1: drafts drawn from their distributions
+    sd_rope              rotary positions with one to four axes
+    sd_kv_append         new rows rotated and written into the target's cache
 """
 
 import ctypes
@@ -33,18 +35,20 @@ __all__ = [
     "sd_semi_ar_draft_workspace_size", "sd_semi_ar_draft",
     "sd_linear_q8", "sd_semi_ar_layer_q8", "sd_avg_pool_compress",
     "sd_latent_compress_q8_workspace_size", "sd_latent_compress_q8",
+    "SD_ROPE_RUNNING", "SD_ROPE_PER_AXIS", "sd_rope", "sd_kv_append",
 ]
 
 SD_OK, SD_ERR_INVALID_ARG, SD_ERR_UNSUPPORTED, SD_ERR_WORKSPACE, SD_ERR_HIP = 0, 1, 2, 3, 4
 SD_F32, SD_BF16 = 0, 1
 SD_ACCEPT_GREEDY, SD_ACCEPT_SAMPLED = 0, 1
+SD_ROPE_RUNNING, SD_ROPE_PER_AXIS = 0, 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 library_path = os.path.join(_HERE, "libspecflash.so")
 _lib = None
 
 _c = ctypes
-_vp, _sz, _i, _f = _c.c_void_p, _c.c_size_t, _c.c_int, _c.c_float
+_vp, _sz, _i, _f, _i64 = _c.c_void_p, _c.c_size_t, _c.c_int, _c.c_float, _c.c_int64
 _SIGNATURES = {
     "sd_status_string": (_c.c_char_p, [_i]),
     "sd_version": (_i, []),
@@ -76,6 +80,8 @@ _SIGNATURES = {
     "sd_latent_compress_q8": (_i, [_vp] * 5 + [_i] * 5 + [_f, _vp, _sz, _vp]),
     "sd_semi_ar_layer_q8": (_i, [_vp] * 18 + [_i] * 7 + [_f, _f, _vp, _sz, _vp]),
     "sd_semi_ar_draft": (_i, [_vp] * 18 + [_i] * 10 + [_f, _f, _f, _vp, _sz, _vp]),
+    "sd_rope": (_i, [_vp, _i64, _vp, _vp, _i64, _i, _i, _i, _i, _vp, _f, _i, _i, _i, _vp]),
+    "sd_kv_append": (_i, [_vp, _i64] * 3 + [_vp] * 6 + [_i, _i, _i, _vp] + [_i] * 6 + [_vp, _f, _i, _i, _i, _vp]),
 }
 
 
@@ -172,6 +178,21 @@ def _same_device(name, t, device):
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
+
+
+def _current(name, t):
+    """The library launches on the current device: tensors of another one are refused."""
+    if t.device.index != _torch()._C._cuda_getDevice():
+        raise ValueError(f"{name} is on {t.device}, which is not the current device")
+
+
+def _pages(num_pages, pool):
+    """Pages a call may use: all of the pool's, or fewer of them."""
+    if num_pages is None:
+        return pool.shape[0]
+    if not 1 <= num_pages <= pool.shape[0]:
+        raise ValueError(f"num_pages must be 1 .. {pool.shape[0]}, the pages of the pool")
+    return num_pages
 
 
 def _stream(stream):
@@ -758,3 +779,130 @@ def sd_avg_pool_compress(feats, C, out=None, stream=None):
     st = library().sd_avg_pool_compress(_ptr(feats), _ptr(out), B, N, C, d, _dtype_code(feats), _stream(stream))
     _raise(st, "sd_avg_pool_compress")
     return out
+
+
+# ---------------------------------------- rotary positions, cache append
+
+def _rows(t, name, dtype=None):
+    """A [T, H, D] tensor whose rows are dense; they may lie any stride apart
+    (a slice of a fused projection).  Returns that stride in elements."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must have 3 dimensions, got {t.dim()}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    T, H, D = t.shape
+    sT, sH, sD = t.stride()
+    if (D > 1 and sD != 1) or (H > 1 and sH != D) or (T > 1 and sT < H * D):
+        raise ValueError(f"{name} must be [T, H, D] with dense rows (any stride between rows)")
+    return sT if T > 1 else H * D
+
+
+def _axes(pos, sections, T, device):
+    """(positions as [axes, T] or None, number of axes, sections as a C array or None)."""
+    torch = _torch()
+    axes = None
+    if pos is not None:
+        _check(pos, "pos", dtype=torch.int32)
+        if pos.dim() not in (1, 2) or pos.shape[-1] != T:
+            raise ValueError(f"pos must be [axes, {T}] or [{T}], got {tuple(pos.shape)}")
+        _same_device("pos", pos, device)
+        axes = pos.shape[0] if pos.dim() == 2 else 1
+    if sections is None:
+        return 1 if axes is None else axes, None
+    n = len(sections)
+    if axes is not None and n != axes:
+        raise ValueError(f"sections must name the pairs of each of the {axes} axes of pos, got {n}")
+    return n, (_c.c_int32 * n)(*sections)
+
+
+def sd_rope(x, pos, theta, sections=None, per_axis=False, inverse=False, out=None, stream=None):
+    """Rotary positions: x [T, H, D] (fp32 or bf16; rows may lie any stride
+    apart), pos [T] or [axes, T] int32, sections the pairs of each axis (None:
+    one axis, all D / 2).  per_axis restarts the frequencies in every section.
+    inverse turns back, which is also the gradient: dx = sd_rope(dy, ...,
+    inverse=True).  out may be x (in place).  Returns out [T, H, D]."""
+    torch = _torch()
+    xs = _rows(x, "x")
+    _current("x", x)
+    dt = _dtype_code(x)
+    T, H, D = x.shape
+    axes, secs = _axes(pos, sections, T, x.device)
+    if out is None:
+        out = torch.empty((T, H, D), dtype=x.dtype, device=x.device)
+    ys = _rows(out, "out", x.dtype)
+    if out.shape != x.shape:
+        raise ValueError(f"out must have shape {tuple(x.shape)}, got {tuple(out.shape)}")
+    _same_device("out", out, x.device)
+    st = library().sd_rope(_ptr(x), xs, _ptr(pos), _ptr(out), ys, T, H, D, axes, secs, float(theta),
+                           SD_ROPE_PER_AXIS if per_axis else SD_ROPE_RUNNING, 1 if inverse else 0, dt,
+                           _stream(stream))
+    _raise(st, "sd_rope")
+    return out
+
+
+def sd_kv_append(q, k, v, k_cache, v_cache, kv_len, theta, pos=None, sections=None, per_axis=False, row_start=None,
+                 page_table=None, num_pages=None, q_out=None, stream=None):
+    """New rows into the cache: k, v [T, Hkv, D] (views of a fused projection
+    allowed), q [T, Hq, D] or None; caches [B, Lmax, Hkv, D], or page pools
+    [P, Hkv, 16, D] with page_table [B, max_pages] int32; kv_len [B] int32, the
+    lengths after the append.  row_start [B + 1] int32 names each sequence's
+    rows (None: T / B rows each, in order).  Keys and queries are rotated at pos
+    [T] or [axes, T] int32 (None: their cache position; theta None: not at
+    all), see sd_rope.  fp32 rows may go into a bf16 cache.  The caches are
+    written in place.  Returns the rotated queries [T, Hq, D] in the cache's
+    dtype (None without q)."""
+    torch = _torch()
+    ks, vs = _rows(k, "k"), _rows(v, "v", k.dtype)
+    _current("k", k)
+    _check(k_cache, "k_cache", ndim=4)
+    _check(v_cache, "v_cache", dtype=k_cache.dtype, ndim=4)
+    _check(kv_len, "kv_len", dtype=torch.int32, ndim=1)
+    T, Hkv, D = k.shape
+    B = kv_len.shape[0]
+    if v.shape != k.shape:
+        raise ValueError("k and v must have the same shape")
+    if k_cache.shape != v_cache.shape:
+        raise ValueError("k_cache and v_cache must have the same shape")
+    dev = k.device
+    if page_table is None:
+        if k_cache.shape[0] != B or k_cache.shape[2] != Hkv or k_cache.shape[3] != D:
+            raise ValueError("contiguous caches must be [B, Lmax, Hkv, D]")
+        Lmax, max_pages, num_pages_ = k_cache.shape[1], 0, 0
+    else:
+        _check(page_table, "page_table", dtype=torch.int32, ndim=2)
+        if (k_cache.shape[1] != Hkv or k_cache.shape[2] != 16 or k_cache.shape[3] != D
+                or page_table.shape[0] != B):
+            raise ValueError("paged caches must be [P, Hkv, 16, D] with a [B, max_pages] table")
+        Lmax, max_pages = 0, page_table.shape[1]
+        num_pages_ = _pages(num_pages, k_cache)
+    if row_start is not None:
+        _check(row_start, "row_start", dtype=torch.int32, ndim=1)
+        if row_start.shape[0] != B + 1:
+            raise ValueError("row_start must be [B + 1]")
+    elif T % B != 0:
+        raise ValueError("without row_start every sequence has T / B rows")
+    Hq, qs = 0, 0
+    if q is not None:
+        qs = _rows(q, "q", k.dtype)
+        Hq = q.shape[1]
+        if q.shape[0] != T or q.shape[2] != D:
+            raise ValueError("q must be [T, Hq, D] with the rows of k")
+        if q_out is None:
+            q_out = torch.empty((T, Hq, D), dtype=k_cache.dtype, device=dev)
+        _out(q_out, "q_out", (T, Hq, D), k_cache.dtype, dev)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    axes, secs = (0, None) if theta is None else _axes(pos, sections, T, dev)
+    for name, t in (("q", q), ("v", v), ("k_cache", k_cache), ("v_cache", v_cache), ("kv_len", kv_len),
+                    ("row_start", row_start), ("page_table", page_table)):
+        _same_device(name, t, dev)
+    st = library().sd_kv_append(_ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _ptr(q_out), _ptr(k_cache), _ptr(v_cache),
+                                _ptr(row_start), _ptr(kv_len), _ptr(page_table), max_pages, num_pages_, Lmax,
+                                None if theta is None else _ptr(pos), T, B, Hq, Hkv, D, axes, secs,
+                                0.0 if theta is None else float(theta),
+                                SD_ROPE_PER_AXIS if per_axis else SD_ROPE_RUNNING, _dtype_code(k),
+                                _dtype_code(k_cache), _stream(stream))
+    _raise(st, "sd_kv_append")
+    return q_out

@@ -235,4 +235,32 @@ SemiArDraftPlan plan_semi_ar_draft(int B, int r0, int d, int Hq, int Hkv, int I,
                                    int cus);
 hipError_t launch_semi_ar_draft(const SemiArDraftArgs& a, const SemiArDraftPlan& p, hipStream_t s);
 
+// --------------------------------------- rotary positions, cache append
+constexpr int kRopeMaxPairs = 128;   // head size 256 at most
+constexpr int kRopeMaxAxes = 4;
+
+// sd_rope: x is q, y is q_out, Hkv = 0.  Strides are elements between tokens.
+struct RopeArgs {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* q_out;
+  void* k_cache;
+  void* v_cache;
+  long long q_stride, k_stride, v_stride, q_out_stride;
+  const int32_t* row_start;    // [B + 1] first row of each sequence, or NULL: `rows` each
+  const int32_t* kv_len;       // [B]
+  const int32_t* page_table;   // [B, max_pages], or NULL: contiguous
+  const int32_t* pos;          // [axes, T], or NULL: the cache position on every axis
+  int T, B, rows, Hq, Hkv, D;
+  int max_pages, num_pages, capacity;
+  int pairs, axes, end[kRopeMaxAxes];   // pairs that turn; end of each axis's run of pairs
+  int per_axis, inverse;
+  double log_theta;
+  int share, step_head, step_unit;      // set at launch: waves per token, a wave's stride in units
+};
+
+hipError_t launch_rope(const RopeArgs& a, int dtype, int cus, hipStream_t s);
+hipError_t launch_kv_append(const RopeArgs& a, int src_dtype, int dtype, int cus, hipStream_t s);
+
 }  // namespace sd

@@ -707,3 +707,134 @@ int sd_avg_pool_compress(const void* feats, float* out, int B, int N, int C, int
   if (B > 65535 || C > 65535 || N > (1 << 24) || d > (1 << 20)) return SD_ERR_UNSUPPORTED;
   return status_from(sd::launch_avg_pool(feats, out, B, N, C, d, dtype, static_cast<hipStream_t>(stream)));
 }
+
+// ---------------------------------------- rotary positions, cache append
+// the pairs that turn and their axes; false: *status says why
+static bool rope_axes_ok(int D, int num_axes, const int32_t* sections, float theta, int freq, sd::RopeArgs* a,
+                         int* status) {
+  *status = SD_ERR_INVALID_ARG;
+  if (D < 1 || num_axes < 0 || (freq != SD_ROPE_RUNNING && freq != SD_ROPE_PER_AXIS)) return false;
+  if (num_axes > 0 && (!isfinite(theta) || !(theta > 0.f))) return false;
+  if (!sections && (num_axes > 1 || (num_axes == 1 && D % 2 != 0))) return false;
+  if (num_axes <= sd::kRopeMaxAxes) {
+    long long pairs = 0;
+    for (int i = 0; i < num_axes; ++i) {
+      const int n = sections ? sections[i] : D / 2;
+      if (n < 1) return false;
+      pairs += n;
+      if (pairs > D / 2) return false;
+      a->end[i] = (int)pairs;
+    }
+    a->pairs = (int)pairs;
+  }
+  *status = SD_ERR_UNSUPPORTED;
+  if (num_axes > sd::kRopeMaxAxes || D > 2 * sd::kRopeMaxPairs) return false;
+  a->D = D;
+  a->axes = num_axes;
+  a->per_axis = freq == SD_ROPE_PER_AXIS;
+  a->log_theta = num_axes > 0 ? log((double)theta) : 0.0;
+  *status = SD_OK;
+  return true;
+}
+
+// Whether T rows of `xw` bytes every `xs` bytes from x share a byte with rows
+// of `yw` bytes every `ys` bytes from y (rows with different strides: whether
+// their whole ranges meet).
+static bool rows_meet(const void* x, long long xs, long long xw, const void* y, long long ys, long long yw, int T) {
+  const uintptr_t x0 = reinterpret_cast<uintptr_t>(x), y0 = reinterpret_cast<uintptr_t>(y);
+  const uintptr_t x1 = x0 + (uintptr_t)(T - 1) * xs + xw, y1 = y0 + (uintptr_t)(T - 1) * ys + yw;
+  if (x1 <= y0 || y1 <= x0) return false;
+  if (xs != ys) return true;
+  const uintptr_t d = (y0 >= x0 ? y0 - x0 : (uintptr_t)xs - (x0 - y0) % xs) % xs;   // y's row start after x's
+  return d < (uintptr_t)xw || (uintptr_t)xs - d < (uintptr_t)yw;
+}
+
+int sd_rope(const void* x, int64_t x_stride, const int32_t* pos, void* y, int64_t y_stride, int T, int H, int D,
+            int num_axes, const int32_t* sections, float theta, int freq, int inverse, int dtype, void* stream) {
+  if (T < 0 || H < 1 || num_axes < 1 || (dtype != SD_F32 && dtype != SD_BF16)) return SD_ERR_INVALID_ARG;
+  sd::RopeArgs a{};
+  int st = SD_OK;
+  if (!rope_axes_ok(D, num_axes, sections, theta, freq, &a, &st)) return st;
+  if (T > (1 << 30) || H > (1 << 20)) return SD_ERR_UNSUPPORTED;
+  if (T == 0) return SD_OK;
+  const int es = dtype == SD_F32 ? 4 : 2;
+  const int64_t width = (int64_t)H * D;
+  if (!x || !pos || !y || !aligned(x, es) || !aligned(y, es) || !aligned(pos, 4)) return SD_ERR_INVALID_ARG;
+  if (x_stride < width || y_stride < width || x_stride > (int64_t(1) << 32) || y_stride > (int64_t(1) << 32))
+    return SD_ERR_INVALID_ARG;
+  if (!(x == y && x_stride == y_stride) &&
+      rows_meet(x, x_stride * es, width * es, y, y_stride * es, width * es, T))
+    return SD_ERR_INVALID_ARG;
+  a.q = x;
+  a.q_out = y;
+  a.q_stride = x_stride;
+  a.q_out_stride = y_stride;
+  a.pos = pos;
+  a.T = T;
+  a.Hq = H;
+  a.inverse = inverse != 0;
+  return status_from(sd::launch_rope(a, dtype, device_cus(), static_cast<hipStream_t>(stream)));
+}
+
+int sd_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                 void* q_out, void* k_cache, void* v_cache, const int32_t* row_start, const int32_t* kv_len,
+                 const int32_t* page_table, int max_pages, int num_pages, int Lmax, const int32_t* pos, int T, int B,
+                 int Hq, int Hkv, int D, int num_axes, const int32_t* sections, float theta, int freq,
+                 int src_dtype, int dtype, void* stream) {
+  if (T < 0 || B < 1 || Hq < 0 || Hkv < 1 || (dtype != SD_F32 && dtype != SD_BF16) ||
+      (src_dtype != SD_F32 && src_dtype != SD_BF16))
+    return SD_ERR_INVALID_ARG;
+  sd::RopeArgs a{};
+  int st = SD_OK;
+  if (!rope_axes_ok(D, num_axes, sections, theta, freq, &a, &st)) return st;
+  if (page_table) {
+    if (max_pages < 1 || num_pages < 1 || max_pages > (1 << 26) || !aligned(page_table, 4)) return SD_ERR_INVALID_ARG;
+  } else if (Lmax < 1) {
+    return SD_ERR_INVALID_ARG;
+  }
+  if (!row_start && T % B != 0) return SD_ERR_INVALID_ARG;
+  if (T > (1 << 30) || Hq > (1 << 20) || Hkv > (1 << 20) || (src_dtype == SD_BF16 && dtype == SD_F32))
+    return SD_ERR_UNSUPPORTED;
+  if (T == 0) return SD_OK;
+  const int ss = src_dtype == SD_F32 ? 4 : 2, es = dtype == SD_F32 ? 4 : 2;
+  const int64_t qw = (int64_t)Hq * D, kw = (int64_t)Hkv * D;
+  if (!k || !v || !k_cache || !v_cache || !kv_len || (Hq > 0 && (!q || !q_out))) return SD_ERR_INVALID_ARG;
+  if (!aligned(k, ss) || !aligned(v, ss) || !aligned(k_cache, es) || !aligned(v_cache, es) || !aligned(kv_len, 4) ||
+      (row_start && !aligned(row_start, 4)) || (pos && !aligned(pos, 4)))
+    return SD_ERR_INVALID_ARG;
+  const int64_t most = int64_t(1) << 32;
+  if (k_stride < kw || v_stride < kw || k_stride > most || v_stride > most) return SD_ERR_INVALID_ARG;
+  if (Hq > 0) {
+    if (!aligned(q, ss) || !aligned(q_out, es) || q_stride < qw || q_stride > most) return SD_ERR_INVALID_ARG;
+    // q_out may be q itself, in place; else it shares no byte with the rows read
+    if (!(q == q_out && src_dtype == dtype && q_stride == qw) &&
+        rows_meet(q, q_stride * ss, qw * ss, q_out, qw * es, qw * es, T))
+      return SD_ERR_INVALID_ARG;
+    if (rows_meet(k, k_stride * ss, kw * ss, q_out, qw * es, qw * es, T) ||
+        rows_meet(v, v_stride * ss, kw * ss, q_out, qw * es, qw * es, T))
+      return SD_ERR_INVALID_ARG;
+    a.q = q;
+    a.q_out = q_out;
+    a.q_stride = q_stride;
+    a.q_out_stride = qw;
+  }
+  a.k = k;
+  a.v = v;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.row_start = row_start;
+  a.kv_len = kv_len;
+  a.page_table = page_table;
+  a.pos = pos;
+  a.T = T;
+  a.B = B;
+  a.rows = row_start ? 0 : T / B;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.max_pages = max_pages;
+  a.num_pages = num_pages;
+  a.capacity = page_table ? max_pages * 16 : Lmax;
+  return status_from(sd::launch_kv_append(a, src_dtype, dtype, device_cus(), static_cast<hipStream_t>(stream)));
+}
