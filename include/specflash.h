@@ -26,6 +26,8 @@
  *
  *   sd_rope              rotary positions of text, images and video
  *   sd_kv_append         new rows rotated and written into the cache
+ *   sd_verify_shared     verification attention of sequences that share long
+ *                        prefixes
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -616,6 +618,61 @@ int sd_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_strid
                  int max_pages, int num_pages, int Lmax, const int32_t* pos, int T, int B,
                  int Hq, int Hkv, int D, int num_axes, const int32_t* sections, float theta,
                  int freq, int src_dtype, int dtype, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Verification attention of sequences that share long prefixes (several
+ * questions about one video, several answers to one prompt): a prefix is read
+ * and attended once for all sequences of its group.
+ *
+ * The B sequences lie in G groups: group i holds the sequences group_start[i]
+ * .. group_start[i + 1] - 1 (NULL: B / G each).  Every row of a group sees the
+ * group's whole prefix, prefix_len[i] keys, and behind it its sequence's own
+ * keys as in sd_verify_attention; kv_len[b] counts the own keys alone, the k
+ * block entries among them.  For block row j, query head h, g = Hq / Hkv:
+ *
+ *   keys: prefix 0 .. prefix_len[i] - 1, own 0 .. kv_len[b] - k + j,
+ *   s = scale * q[b, j, h] . key,
+ *   out[b, j, h] = sum softmax(s) value,  lse[b, j, h] = log sum exp(s)
+ *
+ * A row with no visible key gets out = 0 and lse = -inf.
+ *
+ *   q           [B, k, Hq, D] dtype  (after RoPE; k = 1: single tokens)
+ *   k_cache, v_cache   own keys: contiguous (page_table == NULL) [B, Lmax, Hkv,
+ *               D] dtype, or page pools [num_pages, Hkv, 16, D]
+ *   kv_len      [B] int32, clamped to [0, capacity]
+ *   page_table  [B, max_pages] int32, or NULL
+ *   k_prefix, v_prefix  prefix keys: contiguous (prefix_table == NULL) [G,
+ *               prefix_Lmax, Hkv, D] dtype, or page pools [prefix_num_pages,
+ *               Hkv, 16, D] (they may be k_cache and v_cache)
+ *   prefix_len  [G] int32, clamped to [0, prefix capacity]
+ *   prefix_table [G, prefix_pages] int32, or NULL
+ *   group_start [G + 1] int32, not decreasing, or NULL (then G divides B); a
+ *               sequence of no group has no prefix, groups may be empty
+ *   out         [B, k, Hq, D] out_dtype
+ *   lse         [B, k, Hq] float32, or NULL when not wanted
+ *   workspace   sd_verify_shared_workspace_size(...) bytes, where a capacity
+ *               is Lmax or 16 * max_pages; its size follows the device as for
+ *               sd_verify_attention
+ * SD_BF16 with out_dtype SD_F32 feeds the probabilities to the second product
+ * as pairs of bf16 (2^-17 of each kept); with out_dtype SD_BF16 as one bf16
+ * each (2^-9, the rounding of out itself), a third less matrix work.  SD_F32
+ * runs in float64 and gives SD_F32.
+ * Requirements: those of sd_verify_attention for k, Hq, Hkv, D, scale and
+ * alignment; 1 <= G <= B; Hq <= 2^16; B k Hq < 2^31; fewer than 2^30 tiles of
+ * 32 keys and 16 to 256 rows over all prefixes and sequences at capacity; else
+ * SD_ERR_UNSUPPORTED (the workspace size is then 0).
+ * ---------------------------------------------------------------------- */
+size_t sd_verify_shared_workspace_size(int B, int k, int Hq, int Hkv, int D, int G,
+                                       int prefix_capacity, int capacity, int dtype);
+
+int sd_verify_shared(const void* q, const void* k_cache, const void* v_cache,
+                     const int32_t* kv_len, const int32_t* page_table, int max_pages,
+                     int num_pages, int Lmax, const void* k_prefix, const void* v_prefix,
+                     const int32_t* prefix_len, const int32_t* prefix_table, int prefix_pages,
+                     int prefix_num_pages, int prefix_Lmax, const int32_t* group_start,
+                     void* out, float* lse, int B, int k, int Hq, int Hkv, int D, int G,
+                     float scale, int dtype, int out_dtype, void* workspace,
+                     size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

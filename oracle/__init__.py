@@ -40,7 +40,7 @@ enumeration or brute force.
 """
 
 from .compress import latent_compress, softmax_rows, avg_pool_compress, latent_compress_q8, dequantize_pow2_rows
-from .verify import verify_attention, gather_paged, merge_partials
+from .verify import verify_attention, gather_paged, merge_partials, verify_shared
 from .lm_head import lm_head_logits, softmax_temperature, lm_head_probs, sample_tokens
 from .accept_logits import philox4x64, philox_uniforms, spec_accept_logits
 from .draft_layer import (rms_norm, rope, linear, silu, swiglu, semi_ar_layer, semi_ar_draft, bf16_round,
@@ -67,6 +67,7 @@ __all__ = [
     "verify_attention",
     "gather_paged",
     "merge_partials",
+    "verify_shared",
     "spec_accept",
     "spec_accept_one",
     "accept_flags",

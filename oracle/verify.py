@@ -125,3 +125,49 @@ def merge_partials(outs, lses):
     lse = np.where(z > 0, safe_m + np.log(np.where(z > 0, z, 1.0)), -np.inf)
     o = np.sum(w[..., None] * outs, axis=0) / np.where(z > 0, z, 1.0)[..., None]
     return o, lse
+
+
+def verify_shared(q, k_cache, v_cache, kv_len, k_prefix, v_prefix, prefix_len, group_start, scale, page_table=None,
+                  prefix_table=None, page_size=16):
+    """verify_attention of sequences whose cache is a prefix shared by a group
+    followed by keys of their own: every row sees all prefix_len[i] keys of its
+    group i (sequences group_start[i] .. group_start[i + 1] - 1; none outside
+    every group), then its own keys t <= kv_len[b] - k + j.
+
+    Returns (out, lse, spread) in float64; spread is the same average of |V|.
+    """
+    q = np.asarray(q, dtype=np.float64)
+    B, k, Hq, D = q.shape
+    G = len(prefix_len)
+
+    def sequences(cache, table, lens):
+        if table is not None:
+            return gather_paged(cache, table, lens, page_size)
+        cache = np.asarray(cache, dtype=np.float64)
+        return [cache[i, :n] for i, n in enumerate(lens)]
+
+    keys, vals = (sequences(c, page_table, kv_len) for c in (k_cache, v_cache))
+    pk, pv = (sequences(c, prefix_table, prefix_len) for c in (k_prefix, v_prefix))
+    Hkv = np.asarray(k_cache).shape[2 if page_table is None else 1]
+    g = Hq // Hkv
+    out, spread = np.zeros((2, B, k, Hq, D))
+    lse = np.full((B, k, Hq), -np.inf)
+    for b in range(B):
+        mine = [i for i in range(G) if group_start[i] <= b < group_start[i + 1]]
+        for h in range(Hq):
+            K, V = [keys[b][:, h // g]], [vals[b][:, h // g]]
+            if mine:
+                K.insert(0, pk[mine[0]][:, h // g])
+                V.insert(0, pv[mine[0]][:, h // g])
+            P = len(K[0]) if mine else 0
+            K, V = np.concatenate(K), np.concatenate(V)
+            for j in range(k):
+                n = P + max(0, int(kv_len[b]) - k + j + 1)
+                if n == 0:
+                    continue
+                s = scale * (K[:n] @ q[b, j, h])
+                e = np.exp(s - s.max())
+                out[b, j, h] = e @ V[:n] / e.sum()
+                spread[b, j, h] = e @ np.abs(V[:n]) / e.sum()
+                lse[b, j, h] = s.max() + np.log(e.sum())
+    return out, lse, spread

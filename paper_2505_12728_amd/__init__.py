@@ -13,6 +13,7 @@ library is missing or the tensors are not on the GPU, the calls raise.
     sd_sample_tokens     Algorithm 1: drafts drawn from their distributions
     sd_rope              rotary positions with one to four axes
     sd_kv_append         new rows rotated and written into the target's cache
+    sd_verify_shared     verification attention of sequences that share prefixes
 """
 
 import ctypes
@@ -36,6 +37,7 @@ __all__ = [
     "sd_linear_q8", "sd_semi_ar_layer_q8", "sd_avg_pool_compress",
     "sd_latent_compress_q8_workspace_size", "sd_latent_compress_q8",
     "SD_ROPE_RUNNING", "SD_ROPE_PER_AXIS", "sd_rope", "sd_kv_append",
+    "sd_verify_shared_workspace_size", "sd_verify_shared",
 ]
 
 SD_OK, SD_ERR_INVALID_ARG, SD_ERR_UNSUPPORTED, SD_ERR_WORKSPACE, SD_ERR_HIP = 0, 1, 2, 3, 4
@@ -82,6 +84,9 @@ _SIGNATURES = {
     "sd_semi_ar_draft": (_i, [_vp] * 18 + [_i] * 10 + [_f, _f, _f, _vp, _sz, _vp]),
     "sd_rope": (_i, [_vp, _i64, _vp, _vp, _i64, _i, _i, _i, _i, _vp, _f, _i, _i, _i, _vp]),
     "sd_kv_append": (_i, [_vp, _i64] * 3 + [_vp] * 6 + [_i, _i, _i, _vp] + [_i] * 6 + [_vp, _f, _i, _i, _i, _vp]),
+    "sd_verify_shared_workspace_size": (_sz, [_i] * 9),
+    "sd_verify_shared": (_i, [_vp] * 5 + [_i] * 3 + [_vp] * 4 + [_i] * 3 + [_vp] * 3 + [_i] * 6
+                         + [_f, _i, _i, _vp, _sz, _vp]),
 }
 
 
@@ -213,6 +218,23 @@ def _workspace(nbytes, device, given):
     # zero-filled: some entry points keep arrival counters in the workspace
     # that must start at zero (every call returns them to zero)
     return torch.zeros(nbytes, dtype=torch.uint8, device=device), nbytes
+
+
+def _empty(shape, dtype, device, stream):
+    """Memory for a call on `stream`: a given stream's own, so that the
+    allocator reuses it behind that stream's work."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _scratch(nbytes, device, given, stream):
+    """_workspace for calls that keep no counters in it: left as allocated."""
+    if given is not None or nbytes == 0:
+        return _workspace(nbytes, device, given)
+    return _empty(nbytes, _torch().uint8, device, stream), nbytes
 
 
 def _raise(status, where):
@@ -830,7 +852,7 @@ def sd_rope(x, pos, theta, sections=None, per_axis=False, inverse=False, out=Non
     T, H, D = x.shape
     axes, secs = _axes(pos, sections, T, x.device)
     if out is None:
-        out = torch.empty((T, H, D), dtype=x.dtype, device=x.device)
+        out = _empty((T, H, D), x.dtype, x.device, stream)
     ys = _rows(out, "out", x.dtype)
     if out.shape != x.shape:
         raise ValueError(f"out must have shape {tuple(x.shape)}, got {tuple(out.shape)}")
@@ -890,7 +912,7 @@ def sd_kv_append(q, k, v, k_cache, v_cache, kv_len, theta, pos=None, sections=No
         if q.shape[0] != T or q.shape[2] != D:
             raise ValueError("q must be [T, Hq, D] with the rows of k")
         if q_out is None:
-            q_out = torch.empty((T, Hq, D), dtype=k_cache.dtype, device=dev)
+            q_out = _empty((T, Hq, D), k_cache.dtype, dev, stream)
         _out(q_out, "q_out", (T, Hq, D), k_cache.dtype, dev)
     elif q_out is not None:
         raise ValueError("q_out without q")
@@ -906,3 +928,98 @@ def sd_kv_append(q, k, v, k_cache, v_cache, kv_len, theta, pos=None, sections=No
                                 _dtype_code(k_cache), _stream(stream))
     _raise(st, "sd_kv_append")
     return q_out
+
+
+# ------------------------------------------- verify with shared prefixes
+
+def sd_verify_shared_workspace_size(B, k, Hq, Hkv, D, G, prefix_capacity, capacity, dtype):
+    return library().sd_verify_shared_workspace_size(B, k, Hq, Hkv, D, G, prefix_capacity, capacity, dtype)
+
+
+def _cache_shape(k, v, rows, table, D, dtype, names, device, num_pages=None):
+    """Checks a contiguous cache [rows, L, Hkv, D] or page pools [P, Hkv, 16,
+    D] with their table [rows, pages].  Returns (Hkv, capacity, pages of the
+    table, pages of the pool, L)."""
+    _check(k, names[0], dtype=dtype, ndim=4)
+    _check(v, names[1], dtype=dtype, ndim=4)
+    if k.shape != v.shape:
+        raise ValueError(f"{names[0]} and {names[1]} must have the same shape")
+    for name, t in zip(names, (k, v, table)):
+        _same_device(name, t, device)
+    if table is None:
+        if k.shape[0] != rows or k.shape[3] != D:
+            raise ValueError(f"contiguous {names[0]} must be [{rows}, L, Hkv, {D}], got {tuple(k.shape)}")
+        return k.shape[2], k.shape[1], 0, 0, k.shape[1]
+    _check(table, names[2], dtype=_torch().int32, ndim=2)
+    if k.shape[2] != 16 or k.shape[3] != D or table.shape[0] != rows:
+        raise ValueError(f"paged {names[0]} must be [P, Hkv, 16, {D}] with {names[2]} [{rows}, pages]")
+    return k.shape[1], 16 * table.shape[1], table.shape[1], _pages(num_pages, k), 0
+
+
+def sd_verify_shared(q, k_cache, v_cache, kv_len, prefix_len, k_prefix=None, v_prefix=None, prefix_table=None,
+                     group_start=None, page_table=None, num_pages=None, scale=None, out_dtype=None, out=None, lse=True,
+                     workspace=None, stream=None):
+    """Verification attention of sequences in groups that share a prefix.
+
+    q [B, k, Hq, D]; own caches [B, Lmax, Hkv, D], or page pools [P, Hkv, 16,
+    D] with page_table [B, max_pages]; kv_len [B] counts own keys, the block
+    included.  prefix_len [G]; prefixes k_prefix, v_prefix [G, Lmax, Hkv, D], or
+    pages of the same pools (k_prefix None) or of pools of their own with
+    prefix_table [G, pages].  group_start [G + 1] int32 names each group's
+    sequences (None: B / G each).  scale None: 1 / sqrt(D).  out_dtype float32
+    (the default) or, for bf16 inputs, bfloat16.
+    Returns (out [B, k, Hq, D], lse [B, k, Hq] fp32 or None)."""
+    torch = _torch()
+    _check(q, "q", ndim=4)
+    _current("q", q)
+    _check(kv_len, "kv_len", dtype=torch.int32, ndim=1)
+    _check(prefix_len, "prefix_len", dtype=torch.int32, ndim=1)
+    B, k, Hq, D = q.shape
+    G = prefix_len.shape[0]
+    dev = q.device
+    if kv_len.shape[0] != B:
+        raise ValueError("kv_len needs one entry per sequence")
+    if (k_prefix is None) != (v_prefix is None):
+        raise ValueError("k_prefix and v_prefix come together")
+    if k_prefix is None:
+        if page_table is None or prefix_table is None:
+            raise ValueError("without k_prefix the prefixes are pages of the caches: both tables are needed")
+        k_prefix, v_prefix = k_cache, v_cache
+    dt = _dtype_code(q)
+    Hkv, cap, max_pages, num_pages_, Lmax = _cache_shape(k_cache, v_cache, B, page_table, D, q.dtype,
+                                                         ("k_cache", "v_cache", "page_table"), dev, num_pages)
+    Hkv_p, pcap, ppages, pnum, pL = _cache_shape(k_prefix, v_prefix, G, prefix_table, D, q.dtype,
+                                                 ("k_prefix", "v_prefix", "prefix_table"), dev,
+                                                 num_pages if k_prefix is k_cache else None)
+    if Hkv_p != Hkv:
+        raise ValueError("prefixes and caches must have the same KV heads")
+    if group_start is not None:
+        _check(group_start, "group_start", dtype=torch.int32, ndim=1)
+        if group_start.shape[0] != G + 1:
+            raise ValueError("group_start must be [G + 1]")
+    for name, t in (("kv_len", kv_len), ("prefix_len", prefix_len), ("group_start", group_start)):
+        _same_device(name, t, dev)
+    if scale is None:
+        scale = 1.0 / math.sqrt(D)
+    if out_dtype is None:
+        out_dtype = torch.float32 if out is None else out.dtype
+    if out_dtype != torch.float32 and out_dtype != torch.bfloat16:
+        raise TypeError(f"unsupported out_dtype {out_dtype}: use float32 or bfloat16")
+    if out is None:
+        out = _empty((B, k, Hq, D), out_dtype, dev, stream)
+    _out(out, "out", (B, k, Hq, D), out_dtype, dev)
+    lse_t = None
+    if lse is True:
+        lse_t = _empty((B, k, Hq), torch.float32, dev, stream)
+    elif lse is not None and lse is not False:
+        lse_t = _out(lse, "lse", (B, k, Hq), torch.float32, dev)
+    ws_bytes = sd_verify_shared_workspace_size(B, k, Hq, Hkv, D, G, pcap, cap, dt)
+    ws, ws_len = _scratch(ws_bytes, dev, workspace, stream)
+    st = library().sd_verify_shared(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(kv_len), _ptr(page_table), max_pages,
+                                    num_pages_, Lmax, _ptr(k_prefix), _ptr(v_prefix), _ptr(prefix_len),
+                                    _ptr(prefix_table), ppages, pnum, pL, _ptr(group_start), _ptr(out), _ptr(lse_t),
+                                    B, k, Hq, Hkv, D, G, float(scale), dt,
+                                    SD_F32 if out_dtype == torch.float32 else SD_BF16, _ptr(ws), ws_len,
+                                    _stream(stream))
+    _raise(st, "sd_verify_shared")
+    return out, lse_t

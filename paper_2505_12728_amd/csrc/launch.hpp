@@ -263,4 +263,42 @@ struct RopeArgs {
 hipError_t launch_rope(const RopeArgs& a, int dtype, int cus, hipStream_t s);
 hipError_t launch_kv_append(const RopeArgs& a, int src_dtype, int dtype, int cus, hipStream_t s);
 
+// ------------------------------------------- verify with shared prefixes
+struct SharedPlan {
+  int rows_wg;          // query rows per work-group
+  int rows_own;         // rows of a partial of a sequence's own cache
+  int wgs;              // grid of the stream kernel
+  long long own_base;   // first such row among the partials
+  size_t part_rows;
+  size_t workspace_bytes;
+  bool ok;              // false: the shape exceeds the kernels' index range
+};
+
+struct SharedArgs {
+  const void* q;              // [B, k, Hq, D]
+  const void* k_cache;        // own keys: [B, Lmax, Hkv, D] or pages
+  const void* v_cache;
+  const void* k_prefix;       // prefix keys: [G, prefix_cap, Hkv, D] or pages
+  const void* v_prefix;
+  const int32_t* kv_len;      // [B]
+  const int32_t* prefix_len;  // [G]
+  const int32_t* group_start; // [G + 1], or NULL: B / G sequences each
+  const int32_t* page_table;  // [B, max_pages], or NULL
+  const int32_t* prefix_table;// [G, prefix_pages], or NULL
+  int max_pages, num_pages, Lmax, cap;
+  int prefix_pages, prefix_num_pages, prefix_cap;
+  void* out;                  // [B, k, Hq, D] fp32, or bf16
+  float* lse;                 // [B, k, Hq] or NULL
+  bool out_bf16;
+  int B, k, Hq, Hkv, D, G;
+  float scale, scale_log2;
+  float* part_o;              // [part_rows, D] partial outputs (normalised)
+  float* part_lse;            // [part_rows] partial log-sum-exp (log2 units)
+  int rows_own;
+  long long own_base;
+};
+
+SharedPlan plan_shared(int B, int k, int Hq, int Hkv, int D, int G, int prefix_cap, int cap, int dtype, int cus);
+hipError_t launch_shared(const SharedArgs& a, const SharedPlan& p, int dtype, hipStream_t s);
+
 }  // namespace sd

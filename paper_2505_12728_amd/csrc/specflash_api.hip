@@ -838,3 +838,88 @@ int sd_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_strid
   a.capacity = page_table ? max_pages * 16 : Lmax;
   return status_from(sd::launch_kv_append(a, src_dtype, dtype, device_cus(), static_cast<hipStream_t>(stream)));
 }
+
+// ------------------------------------------- verify with shared prefixes
+static bool shared_shape_ok(int B, int k, int Hq, int Hkv, int D, int G, int prefix_cap, int cap, int dtype,
+                            int* status) {
+  if (!verify_shape_ok(B, k, Hq, Hkv, D, dtype, status)) return false;
+  *status = SD_ERR_INVALID_ARG;
+  if (G < 1 || prefix_cap < 1 || cap < 1) return false;
+  *status = SD_ERR_UNSUPPORTED;
+  if (G > B || Hq > (1 << 16) || (long long)B * k * Hq >= (1LL << 31)) return false;
+  *status = SD_OK;
+  return true;
+}
+
+size_t sd_verify_shared_workspace_size(int B, int k, int Hq, int Hkv, int D, int G, int prefix_capacity, int capacity,
+                                       int dtype) {
+  int st;
+  if (!shared_shape_ok(B, k, Hq, Hkv, D, G, prefix_capacity, capacity, dtype, &st)) return 0;
+  const sd::SharedPlan plan = sd::plan_shared(B, k, Hq, Hkv, D, G, prefix_capacity, capacity, dtype, device_cus());
+  return plan.ok ? plan.workspace_bytes : 0;
+}
+
+int sd_verify_shared(const void* q, const void* k_cache, const void* v_cache, const int32_t* kv_len,
+                     const int32_t* page_table, int max_pages, int num_pages, int Lmax, const void* k_prefix,
+                     const void* v_prefix, const int32_t* prefix_len, const int32_t* prefix_table, int prefix_pages,
+                     int prefix_num_pages, int prefix_Lmax, const int32_t* group_start, void* out, float* lse, int B,
+                     int k, int Hq, int Hkv, int D, int G, float scale, int dtype, int out_dtype, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+  constexpr int most_pages = 1 << 26;
+  if (page_table ? max_pages < 1 || num_pages < 1 || max_pages > most_pages || !aligned(page_table, 4) : Lmax < 1)
+    return SD_ERR_INVALID_ARG;
+  if (prefix_table ? prefix_pages < 1 || prefix_num_pages < 1 || prefix_pages > most_pages || !aligned(prefix_table, 4)
+                   : prefix_Lmax < 1)
+    return SD_ERR_INVALID_ARG;
+  const int cap = page_table ? max_pages * 16 : Lmax;
+  const int prefix_cap = prefix_table ? prefix_pages * 16 : prefix_Lmax;
+  int st = SD_OK;
+  if (!shared_shape_ok(B, k, Hq, Hkv, D, G, prefix_cap, cap, dtype, &st)) return st;
+  if (!q || !k_cache || !v_cache || !kv_len || !k_prefix || !v_prefix || !prefix_len || !out || !isfinite(scale) ||
+      (out_dtype != SD_F32 && out_dtype != SD_BF16))
+    return SD_ERR_INVALID_ARG;
+  if (dtype == SD_F32 && out_dtype == SD_BF16) return SD_ERR_UNSUPPORTED;
+  if (!group_start && B % G != 0) return SD_ERR_INVALID_ARG;
+  const size_t al = dtype == SD_BF16 ? 16 : 4;
+  if (!aligned(q, al) || !aligned(k_cache, al) || !aligned(v_cache, al) || !aligned(k_prefix, al) ||
+      !aligned(v_prefix, al) || !aligned(out, out_dtype == SD_BF16 ? 8 : 16) || !aligned(kv_len, 4) ||
+      !aligned(prefix_len, 4) || (group_start && !aligned(group_start, 4)) || (lse && !aligned(lse, 4)))
+    return SD_ERR_INVALID_ARG;
+  const sd::SharedPlan plan = sd::plan_shared(B, k, Hq, Hkv, D, G, prefix_cap, cap, dtype, device_cus());
+  if (!plan.ok) return SD_ERR_UNSUPPORTED;
+  if (!workspace || workspace_bytes < plan.workspace_bytes || !aligned(workspace, 16)) return SD_ERR_WORKSPACE;
+  sd::SharedArgs a{};
+  a.q = q;
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.k_prefix = k_prefix;
+  a.v_prefix = v_prefix;
+  a.kv_len = kv_len;
+  a.prefix_len = prefix_len;
+  a.group_start = group_start;
+  a.page_table = page_table;
+  a.prefix_table = prefix_table;
+  a.max_pages = max_pages;
+  a.num_pages = num_pages;
+  a.Lmax = Lmax;
+  a.cap = cap;
+  a.prefix_pages = prefix_pages;
+  a.prefix_num_pages = prefix_num_pages;
+  a.prefix_cap = prefix_cap;
+  a.out = out;
+  a.lse = lse;
+  a.out_bf16 = out_dtype == SD_BF16;
+  a.B = B;
+  a.k = k;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.D = D;
+  a.G = G;
+  a.scale = scale;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.part_o = static_cast<float*>(workspace);
+  a.part_lse = a.part_o + plan.part_rows * D;
+  a.rows_own = plan.rows_own;
+  a.own_base = plan.own_base;
+  return status_from(sd::launch_shared(a, plan, dtype, static_cast<hipStream_t>(stream)));
+}

@@ -101,3 +101,54 @@ def test_append_overlapping_queries_refused(append):
     assert append(qo=q, sdt=0) == sd.SD_ERR_INVALID_ARG          # fp32 rows, bf16 output in their place
     assert append(qo=k) == sd.SD_ERR_INVALID_ARG
     assert append(qo=append.base["v"]) == sd.SD_ERR_INVALID_ARG
+
+
+@pytest.fixture
+def shared(lib):
+    keep, (q, kc, vc, kl, pt, kp, vp, pl, ppt, gs, out, lse, ws) = _fake(13)
+    base = dict(q=q, kc=kc, vc=vc, kl=kl, pt=None, mp=0, npg=0, lmax=64, kp=kp, vp=vp, pl=pl, ppt=None, pp=0, pn=0,
+                plm=96, gs=None, out=out, lse=lse, B=4, k=4, Hq=8, Hkv=2, D=128, G=2, scale=0.1, dt=1, odt=0, ws=ws,
+                wsb=1 << 34)
+    order = list(base)
+
+    def call(**kw):
+        a = dict(base, **kw)
+        return lib.sd_verify_shared(*[a[n] for n in order], None)
+    call.base, call.keep = base, keep
+    return call
+
+
+@pytest.mark.parametrize("bad", [
+    dict(q=None), dict(kc=None), dict(vc=None), dict(kl=None), dict(kp=None), dict(vp=None), dict(pl=None),
+    dict(out=None), dict(B=0), dict(k=0), dict(Hq=6, Hkv=4), dict(G=0), dict(G=3), dict(lmax=0), dict(plm=0),
+    dict(dt=2), dict(odt=2), dict(scale=float("nan")), dict(scale=float("inf"))])
+def test_shared_invalid(shared, bad):
+    assert shared(**bad) == sd.SD_ERR_INVALID_ARG
+
+
+def test_shared_unsupported(shared, lib):
+    for bad in (dict(k=17), dict(D=96), dict(Hq=512, Hkv=1), dict(dt=0, Hq=32, Hkv=1), dict(G=5), dict(dt=0, odt=1),
+                dict(B=1 << 20, G=1 << 20, lmax=1 << 20), dict(B=1 << 28, Hq=8, Hkv=8, G=1),
+                dict(Hq=1 << 17, Hkv=1 << 17)):
+        assert shared(**bad) == sd.SD_ERR_UNSUPPORTED, bad
+    assert lib.sd_verify_shared_workspace_size(1 << 20, 4, 8, 2, 128, 1, 64, 1 << 20, 1) == 0
+    assert lib.sd_verify_shared_workspace_size(4, 4, 8, 2, 128, 5, 64, 64, 1) == 0
+    assert lib.sd_verify_shared_workspace_size(4, 4, 8, 2, 128, 4, 64, 64, 1) > 0
+
+
+def test_shared_tables_alignment_and_workspace(shared):
+    t = shared.base["kl"]
+    assert shared(pt=t, mp=0, npg=1) == sd.SD_ERR_INVALID_ARG
+    assert shared(pt=t, mp=1, npg=0) == sd.SD_ERR_INVALID_ARG
+    assert shared(ppt=t, pp=0, pn=1) == sd.SD_ERR_INVALID_ARG
+    assert shared(ppt=t, pp=1, pn=0) == sd.SD_ERR_INVALID_ARG
+    assert shared(ppt=t, pp=(1 << 26) + 1, pn=1) == sd.SD_ERR_INVALID_ARG
+    for name in ("q", "kc", "vc", "kp", "vp"):
+        assert shared(**{name: ctypes.c_void_p(shared.base[name].value + 8)}) == sd.SD_ERR_INVALID_ARG, name
+    for name in ("kl", "pl", "lse"):
+        assert shared(**{name: ctypes.c_void_p(shared.base[name].value + 2)}) == sd.SD_ERR_INVALID_ARG, name
+    assert shared(out=ctypes.c_void_p(shared.base["out"].value + 8)) == sd.SD_ERR_INVALID_ARG
+    assert shared(gs=ctypes.c_void_p(t.value + 2)) == sd.SD_ERR_INVALID_ARG
+    assert shared(ws=None) == sd.SD_ERR_WORKSPACE
+    assert shared(wsb=64) == sd.SD_ERR_WORKSPACE
+    assert shared(ws=ctypes.c_void_p(shared.base["ws"].value + 8)) == sd.SD_ERR_WORKSPACE

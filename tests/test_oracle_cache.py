@@ -73,3 +73,25 @@ def test_append_then_gather_is_the_rotated_sequence():
             assert np.allclose(qo[t], oracle.rope_axes(q[t:t + 1], np.array([[p]]), [2], 100.0)[0])
         assert np.all(keys[b][:kv_len[b] - n[b]] == 9.0)
     assert np.isnan(qo[-2:]).all() and np.all(kc[[2, 7]] == 9.0)
+
+
+def test_shared_prefix_equals_separate_caches():
+    g = np.random.default_rng(4)
+    B, k, Hq, Hkv, D, G = 5, 3, 4, 2, 8, 3
+    q = g.standard_normal((B, k, Hq, D))
+    kc, vc = g.standard_normal((2, B, 12, Hkv, D))
+    kp, vp = g.standard_normal((2, G, 9, Hkv, D))
+    kv_len, plen, start = np.array([12, 3, 7, 0, 2]), np.array([9, 4, 0]), np.array([0, 2, 2, 4])
+    out, lse, spread = oracle.verify_shared(q, kc, vc, kv_len, kp, vp, plen, start, 0.3)
+    for b in range(B):
+        i = {0: 0, 1: 0, 2: 2, 3: 2}.get(b)           # group 1 is empty, sequence 4 in none
+        n = 0 if i is None else plen[i]
+        lead = [x[i, :n] if i is not None else x[0, :0] for x in (kp, vp)]
+        K, V = (np.concatenate([a, c[b, :kv_len[b]]])[None] for a, c in zip(lead, (kc, vc)))
+        if kv_len[b] >= k:
+            ro, rl = oracle.verify_attention(q[b:b + 1], K, V, [n + kv_len[b]], 0.3)
+            assert np.allclose(out[b], ro[0]) and np.allclose(lse[b], rl[0])
+    # no own key visible: the prefix alone, or nothing
+    assert np.all(lse[3] == -np.inf) and not out[3].any()
+    assert np.all(np.isinf(lse[4, 0])) and np.all(np.isfinite(lse[4, 1:]))
+    assert np.all(spread >= np.abs(out) - 1e-12)
