@@ -38,7 +38,13 @@
 namespace sd {
 namespace {
 
-constexpr int kTile = 32;   // keys per tile
+
+constexpr int kTileNarrow = 32, kTileWide = 64;   // keys per tile
+// Places of the list in front of a pair's first tile: starting a pair (its
+// queries' latency with the ring drained, the partial of the one before) takes
+// about as long as this many tiles.
+constexpr int kStart = 2;
+constexpr float kHeadroom = 24.f;   // log2 of the largest weight before the maximum is raised
 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) const void gbl_cvoid;
@@ -56,11 +62,15 @@ __device__ __forceinline__ int group_bound(const SharedArgs& a, int g) {
   return min(max(((cint32*)a.group_start)[g], 0), a.B);
 }
 
-__device__ __forceinline__ int tiles_of(int L) { return (L + kTile - 1) / kTile; }
+template <int TK>
+__device__ __forceinline__ int tiles_of(int L) {
+  return (L + TK - 1) / TK;
+}
 __device__ __forceinline__ int row_tiles(int rows, int per) { return (rows + per - 1) / per; }
 
-// Place of a pair in the list
+// A tile of the list
 struct Cursor {
+  int n;             // its place
   int u;             // unit
   int hk, rt, t;     // KV head, row tile, key tile
   int nt, RT;        // key tiles and row tiles of the unit
@@ -71,17 +81,17 @@ struct Cursor {
 // What a scan over the units finds: lane l holds unit u0 + l.
 struct Span {
   Unit un;
-  int tiles, pairs;      // of this unit
-  int t_before, p_before;   // before it, in the whole list / among its kind
+  int places, pairs;        // of this unit
+  int n_before, p_before;   // before it
 };
 
 // Units u0 .. u0 + 63 with their exclusive sums, given the sums and the group
 // bound carried from the units before.  Group bounds are made monotone by a
 // running maximum, so that no sequence is in two groups.
 struct Carry {
-  int tiles = 0, pairs = 0, bound = 0;
+  int places = 0, pairs = 0, bound = 0;
 };
-template <int ROWS>
+template <int ROWS, int TK>
 __device__ __forceinline__ Span scan_units(const SharedArgs& a, int u0, Carry& c) {
   const int lane = threadIdx.x & 63;
   const int u = u0 + lane;
@@ -115,8 +125,8 @@ __device__ __forceinline__ Span scan_units(const SharedArgs& a, int u0, Carry& c
   }
   c.bound = max(c.bound, __shfl(bound, 63, 64));
   s.pairs = a.Hkv * row_tiles(s.un.rows, ROWS);
-  s.tiles = s.pairs * tiles_of(s.un.L);
-  int ti = s.tiles, pi = s.pairs;
+  s.places = s.un.L > 0 ? s.pairs * (tiles_of<TK>(s.un.L) + kStart) : 0;
+  int ti = s.places, pi = s.pairs;
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) {
     const int x = __shfl_up(ti, off, 64), y = __shfl_up(pi, off, 64);
@@ -125,30 +135,30 @@ __device__ __forceinline__ Span scan_units(const SharedArgs& a, int u0, Carry& c
       pi += y;
     }
   }
-  s.t_before = c.tiles + ti - s.tiles;
+  s.n_before = c.places + ti - s.places;
   s.p_before = c.pairs + pi - s.pairs;
-  c.tiles += __shfl(ti, 63, 64);
+  c.places += __shfl(ti, 63, 64);
   c.pairs += __shfl(pi, 63, 64);
   return s;
 }
 
 // length T of the list
-template <int ROWS>
-__device__ __forceinline__ int total_tiles(const SharedArgs& a) {
+template <int ROWS, int TK>
+__device__ __forceinline__ int list_length(const SharedArgs& a) {
   Carry c;
-  for (int u0 = 0; u0 < a.G + a.B; u0 += 64) scan_units<ROWS>(a, u0, c);
-  return c.tiles;
+  for (int u0 = 0; u0 < a.G + a.B; u0 += 64) scan_units<ROWS, TK>(a, u0, c);
+  return c.places;
 }
 
-// cursor of tile n of the list (0 <= n < T); wave-uniform, in scalar registers.
-// The pair counts its kind only: own pairs start at 0 again (R rows each).
-template <int ROWS>
-__device__ __forceinline__ Cursor locate(const SharedArgs& a, int n) {
+// cursor of the first tile at place n (0 <= n < T) or behind it.  The pair counts
+// its kind only: own pairs start at 0 again (R rows each).
+template <int ROWS, int TK>
+__device__ __forceinline__ Cursor find_tile(const SharedArgs& a, int n) {
   Carry c;
   for (int u0 = 0; u0 < a.G + a.B; u0 += 64) {
-    const Span s = scan_units<ROWS>(a, u0, c);
-    if (n >= c.tiles) continue;
-    const int f = __builtin_ctzll(__ballot(s.t_before + s.tiles > n));
+    const Span s = scan_units<ROWS, TK>(a, u0, c);
+    if (n >= c.places) continue;
+    const int f = __builtin_ctzll(__ballot(s.n_before + s.places > n));
     auto of = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
     Cursor cu;
     cu.u = u0 + f;
@@ -156,11 +166,12 @@ __device__ __forceinline__ Cursor locate(const SharedArgs& a, int n) {
     cu.rows = of(s.un.rows);
     cu.first = of(s.un.first);
     cu.end = of(s.un.end);
-    cu.nt = tiles_of(cu.L);
+    cu.nt = tiles_of<TK>(cu.L);
     cu.RT = row_tiles(cu.rows, ROWS);
-    const int rem = n - of(s.t_before);
-    const int x = rem / cu.nt;
-    cu.t = rem - x * cu.nt;
+    const int rem = n - of(s.n_before);
+    const int x = rem / (cu.nt + kStart);
+    cu.t = max(rem - x * (cu.nt + kStart) - kStart, 0);
+    cu.n = of(s.n_before) + x * (cu.nt + kStart) + kStart + cu.t;
     cu.hk = x / cu.RT;
     cu.rt = x - cu.hk * cu.RT;
     cu.pair = cu.u < a.G ? of(s.p_before) + x : (cu.u - a.G) * a.Hkv * cu.RT + x;
@@ -169,11 +180,29 @@ __device__ __forceinline__ Cursor locate(const SharedArgs& a, int n) {
   return Cursor{};   // n >= T: not reached
 }
 
+// the same in scalar registers (the compiler cannot see that the search ends
+// alike on every lane), so that its bookkeeping stays off the vector unit
+template <int ROWS, int TK>
+__device__ __forceinline__ Cursor locate(const SharedArgs& a, int n) {
+  Cursor cu = find_tile<ROWS, TK>(a, n);
+  int* f[] = {&cu.n, &cu.u, &cu.hk, &cu.rt, &cu.t, &cu.nt, &cu.RT, &cu.L, &cu.rows, &cu.first, &cu.end, &cu.pair};
+#pragma unroll
+  for (int* x : f) *x = __builtin_amdgcn_readfirstlane(*x);
+  return cu;
+}
+
+// place of the tile behind cu
+__device__ __forceinline__ int place_behind(const Cursor& cu) {
+  return cu.n + 1 + (cu.t + 1 == cu.nt ? kStart : 0);
+}
+
 // next tile of the list; the caller never steps past the last one
-template <int ROWS>
+template <int ROWS, int TK>
 __device__ __forceinline__ void advance(const SharedArgs& a, Cursor& cu) {
+  ++cu.n;
   if (++cu.t < cu.nt) return;
   cu.t = 0;
+  cu.n += kStart;
   ++cu.pair;
   if (++cu.rt < cu.RT) return;
   cu.rt = 0;
@@ -193,7 +222,7 @@ __device__ __forceinline__ void advance(const SharedArgs& a, Cursor& cu) {
       cu.rows = a.k * (a.Hq / a.Hkv);
       cu.L = cu.first < a.B ? min(max(((cint32*)a.kv_len)[cu.first], 0), a.cap) : 0;
     }
-    cu.nt = tiles_of(cu.L);
+    cu.nt = tiles_of<TK>(cu.L);
     cu.RT = row_tiles(cu.rows, ROWS);
     if (cu.nt == 0 || cu.RT == 0) cu.pair += a.Hkv * cu.RT;
   } while ((cu.nt == 0 || cu.RT == 0) && cu.u < a.G + a.B);
@@ -217,7 +246,7 @@ __device__ __forceinline__ int out_row(const SharedArgs& a, int first, int hk, i
 // ------------------------------------------------------------ bf16 stream
 template <int D, int NW, int RB, int NBUF, bool HILO>
 __global__ __launch_bounds__(NW * 64, 2) void shared_stream_bf16(SharedArgs a, int G) {
-  constexpr int TK = kTile;
+  constexpr int TK = kTileNarrow;
   constexpr int DC = D / 32;                   // 32-channel slices (S^T = K Q^T)
   constexpr int DB = D / 16;                   // 16-channel blocks (O^T)
   constexpr int PK = D / 8;                    // 16-byte pieces per key row
@@ -229,16 +258,16 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_stream_bf16(SharedArgs a, i
   constexpr int ROWS = NW * RB * 16;
   static_assert((2 * DMA_PER_HALF) % NW == 0, "tile copy must split evenly");
   static_assert(NBUF >= 3 && (NBUF - 2) * DMA_PER_WAVE < 64, "ring depth and vmcnt range");
-  constexpr float kRescale = 8.f;              // log2 headroom before rescaling
   __shared__ __align__(16) unsigned char ring[NBUF][BUF_BYTES];
 
   const int lane = threadIdx.x & 63, G4 = lane >> 4, c = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wg = blockIdx.x;
-  const int T = __builtin_amdgcn_readfirstlane(total_tiles<ROWS>(a));
+  const int T = __builtin_amdgcn_readfirstlane(list_length<ROWS, TK>(a));
   const int n0 = (int)((long long)T * wg / G), n1 = (int)((long long)T * (wg + 1) / G);
   if (n0 >= n1) return;
-  const int last = n1 - 1;
+  Cursor cc = locate<ROWS, TK>(a, n0);
+  if (cc.n >= n1) return;
 
   // copies: copy i of this wave covers pieces P of K or V: key P / PK, LDS slot
   // P % PK holding global piece slot ^ lds_swizzle(key)
@@ -403,13 +432,13 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_stream_bf16(SharedArgs a, i
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       // Exponents before the mask: their largest bounds the masked ones, so
-      // that m, raised only when a lane passes 2^8, may exceed the true maximum;
+      // that m, raised only when a lane passes 2^24, may exceed the true maximum;
       // it cancels in o = O / l and lse = m + log2 l.
       float y[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] = fmaf(x[rb][e], sl2, -m[rb]);
       const float ly = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
-      if (__ballot(ly > kRescale) != 0ull) {
+      if (__ballot(ly > kHeadroom) != 0ull) {
         const float lm = fmaxf(fmaxf(fmaxf(x[rb][0], x[rb][1]), fmaxf(x[rb][2], x[rb][3])),
                                fmaxf(fmaxf(x[rb][4], x[rb][5]), fmaxf(x[rb][6], x[rb][7])));
         const float mnew = fmaxf(m[rb], wave_max_across_groups(lm) * sl2);
@@ -461,38 +490,408 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_stream_bf16(SharedArgs a, i
   // that at each wait exactly NBUF - 2 tiles' copies are newer than the step's
   // own; the barrier also frees the previous step's slot.  A new segment drains
   // this wave's memory counter, so that the counted waits only see copies.
-  Cursor cc = locate<ROWS>(a, n0);
   Cursor ic = cc;
-  int in = n0;
+  auto copy_next = [&](int slot) {
+    issue(ic, ring[slot]);
+    if (place_behind(ic) < n1) advance<ROWS, TK>(a, ic);
+  };
 #pragma unroll 1
-  for (int i = 0; i < NBUF - 1; ++i) {
-    issue(ic, ring[i]);
-    if (in < last) {
-      advance<ROWS>(a, ic);
-      ++in;
-    }
-  }
+  for (int i = 0; i < NBUF - 1; ++i) copy_next(i);
   bool fresh = true;
 #pragma unroll 1
-  for (int n = n0; n < n1; ++n) {
-    const int s = n - n0;
+  for (int s = 0;; ++s) {
     wait_vm_then_barrier<(NBUF - 2) * DMA_PER_WAVE>();
-    issue(ic, ring[(s + NBUF - 1) % NBUF]);
-    if (in < last) {
-      advance<ROWS>(a, ic);
-      ++in;
-    }
+    copy_next((s + NBUF - 1) % NBUF);
     if (fresh) {
-      if (n != n0) flush();
+      if (s != 0) flush();
       start_segment(cc);
       __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));   // vmcnt(0)
     }
     if (busy) compute(cc.t * TK, ring[s % NBUF]);
     fresh = cc.t + 1 == cc.nt;
-    if (n < last) advance<ROWS>(a, cc);
+    if (place_behind(cc) >= n1) break;
+    advance<ROWS, TK>(a, cc);
   }
   __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));   // no copy may still write this LDS
   flush();
+}
+
+// ------------------------------------------------- bf16 stream, many rows
+// Eight waves of RB 16-row blocks on 64-key tiles, matrix-core bound.  A step
+// computes the scores of tile x + 1 under the exponentials of tile x, then P V
+// of tile x under the row maxima of tile x + 1, which are raised (rarely) after
+// it.  It runs in groups of four LDS fragments each: a group's reads are issued
+// one group ahead and waited for by count, and its matrix-core and vector
+// operations alternate.  K and V have rings of four slots; the tile that a step
+// copies lands two steps later.
+template <int ID, int MFMAS, int VALUS>
+__device__ __forceinline__ void alternate() {
+  if constexpr (MFMAS > 0) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, ID);
+    __builtin_amdgcn_sched_group_barrier(0x002, VALUS, ID);
+    alternate<ID, MFMAS - 1, VALUS>();
+  }
+}
+
+template <int V>
+struct Const {
+  static constexpr int value = V;
+};
+template <int I, int N, typename F>
+__device__ __forceinline__ void unrolled(F&& f) {
+  if constexpr (I < N) {
+    f(Const<I>{});
+    unrolled<I + 1, N>(f);
+  }
+}
+
+template <int D, int RB, bool HILO>
+__global__ __launch_bounds__(512, 2) void shared_wide_bf16(SharedArgs a, int G) {
+  constexpr int NW = 8, TK = kTileWide, NBUF = 4;
+  constexpr int DC = D / 32;                   // 32-channel slices (S^T = K Q^T)
+  constexpr int DB = D / 16;                   // 16-channel blocks (O^T)
+  constexpr int PK = D / 8;                    // 16-byte pieces per key row
+  constexpr int ROW = D * 2;
+  constexpr int HALF = TK * ROW;               // a tile's K (or V)
+  constexpr int KEYS = 64 / PK;                // keys of one 64-lane copy
+  constexpr int COPIES = TK / KEYS / NW;       // per wave and half
+  constexpr int ROWS = NW * RB * 16;
+  constexpr int KPG = 4 / DC;                  // 16-key blocks of a score group
+  constexpr int NQK = 4 / KPG, NPVH = DB / 4, NG = NQK + 2 * NPVH;
+  static_assert(NBUF * HALF <= 65536, "ring slots within the LDS instructions' offsets");
+  __shared__ __align__(16) unsigned char ring[2][NBUF * HALF];   // K, V
+
+  const int lane = threadIdx.x & 63, G4 = lane >> 4, c = lane & 15;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wg = blockIdx.x;
+  const int T = __builtin_amdgcn_readfirstlane(list_length<ROWS, TK>(a));
+  const int n0 = (int)((long long)T * wg / G), n1 = (int)((long long)T * (wg + 1) / G);
+  if (n0 >= n1) return;
+  Cursor cc = locate<ROWS, TK>(a, n0);
+  if (cc.n >= n1) return;
+
+  // copy i of this wave takes keys (w COPIES + i) KEYS .. of K and of V; a lane's
+  // 16-byte piece goes to LDS slot piece ^ lds_swizzle(key).  A copy's keys lie in
+  // one page.  Keys past the unit's length re-read its last key (masked).
+  int ckey[COPIES];
+  uint32_t cpiece[COPIES];
+#pragma unroll
+  for (int i = 0; i < COPIES; ++i) {
+    ckey[i] = (w * COPIES + i) * KEYS + lane / PK;
+    cpiece[i] = ((lane % PK) ^ lds_swizzle<PK>(ckey[i])) * 16;
+  }
+  // the tile that is copied next: its first keys' byte offsets in the caches
+  // (found one step ahead, as page ids are loads) and its last key
+  size_t cbase[COPIES];
+  int clast = 0, cstep = 0;
+  const unsigned char *ck = nullptr, *cv = nullptr;
+  auto place = [&](const Cursor& cu) {
+    const bool own = cu.u >= a.G;
+    const int row = own ? cu.first : cu.u;
+    ck = static_cast<const unsigned char*>(own ? a.k_cache : a.k_prefix);
+    cv = static_cast<const unsigned char*>(own ? a.v_cache : a.v_prefix);
+    const int32_t* table = own ? a.page_table : a.prefix_table;
+    const int t0 = cu.t * TK;
+    clast = cu.L - 1 - t0;
+    if (table != nullptr) {
+      const int pages = own ? a.num_pages : a.prefix_num_pages;
+      cint32* pt = (cint32*)(table + (size_t)row * (own ? a.max_pages : a.prefix_pages));
+      const int lastp = (cu.L - 1) >> 4;
+      cstep = ROW;
+#pragma unroll
+      for (int i = 0; i < COPIES; ++i) {
+        const int key0 = (w * COPIES + i) * KEYS;
+        const int pi = min((t0 + key0) >> 4, lastp);
+        const int page = min(max((int)pt[pi], 0), pages - 1);
+        // offset of the tile's key 0 as if every key lay in this page
+        cbase[i] = (((size_t)page * a.Hkv + cu.hk) * 16) * ROW - (size_t)(pi * 16 - t0) * ROW;
+      }
+    } else {
+      cstep = a.Hkv * ROW;
+#pragma unroll
+      for (int i = 0; i < COPIES; ++i)
+        cbase[i] = (((size_t)row * (own ? a.Lmax : a.prefix_cap) + t0) * a.Hkv + cu.hk) * ROW;
+    }
+  };
+  auto issue = [&](int slot) {
+#pragma unroll
+    for (int i = 0; i < COPIES; ++i) {
+      const uint32_t off = (uint32_t)min(ckey[i], clast) * (uint32_t)cstep + cpiece[i];
+      const int at = slot * HALF + (w * COPIES + i) * 1024;
+      __builtin_amdgcn_global_load_lds((gbl_cvoid*)(ck + cbase[i] + off), (lds_void*)(ring[0] + at), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((gbl_cvoid*)(cv + cbase[i] + off), (lds_void*)(ring[1] + at), 16, 0, 0);
+    }
+  };
+
+  // fragment addresses for the first 16 keys of slot 0 (the swizzle depends on
+  // key % 16 only, so further blocks and slots are offsets)
+  uint32_t kaddr[DC], vaddr[DB];
+#pragma unroll
+  for (int dc = 0; dc < DC; ++dc)
+    kaddr[dc] = lds_addr(ring[0]) + c * ROW + (((dc * 4 + G4) ^ lds_swizzle<PK>(c)) * 16);
+#pragma unroll
+  for (int db = 0; db < DB; ++db) {
+    const int key = 4 * G4 + (c >> 2), ch = db * 16 + 4 * (c & 3);
+    vaddr[db] = lds_addr(ring[1]) + key * ROW + (((ch >> 3) ^ lds_swizzle<PK>(key)) * 16) + (ch & 7) * 2;
+  }
+
+  // segment state (rows, maxima and sums as in the narrow kernel)
+  bf16x8 qf[RB][DC];
+  int lim[RB];
+  float m[RB], l[RB];
+  floatx4 o[RB][DB], sc[4][RB];                // sc: raw scores of the tile whose turn it is
+  const bool neg = a.scale_log2 < 0.f;
+  const float sl2 = fabsf(a.scale_log2);
+  const int g = a.Hq / a.Hkv, kg = a.k * g;
+
+  u32x4 xr[2][4];
+  u32x2 vr[2][4][2];
+  // LDS reads of group gr, or the ties that make their values usable
+  auto reads = [&](auto gtag, auto ph_next, auto ph_here, uint32_t dn, uint32_t dh, auto tie_only) {
+    constexpr int gr = decltype(gtag)::value, PN = decltype(ph_next)::value, PH = decltype(ph_here)::value;
+    if constexpr (gr < NQK) {
+      unrolled<0, 4>([&](auto jt) {
+        constexpr int j = decltype(jt)::value, kb = gr * KPG + j / DC;
+        if constexpr (decltype(tie_only)::value)
+          tie(xr[gr & 1][j]);
+        else
+          xr[gr & 1][j] = lds_read_b128_off<PN * HALF + kb * 16 * ROW>(kaddr[j % DC] + dn);
+      });
+    } else if constexpr (gr < NG) {
+      constexpr int q = gr - NQK, hf = q / NPVH, pb = q % NPVH;
+      unrolled<0, 4>([&](auto dt) {
+        constexpr int d = decltype(dt)::value;
+        if constexpr (decltype(tie_only)::value) {
+          tie(vr[gr & 1][d][0]);
+          tie(vr[gr & 1][d][1]);
+        } else {
+          vr[gr & 1][d][0] = lds_read_tr16_b64_off<PH * HALF + hf * 32 * ROW>(vaddr[4 * pb + d] + dh);
+          vr[gr & 1][d][1] = lds_read_tr16_b64_off<PH * HALF + hf * 32 * ROW + 16 * ROW>(vaddr[4 * pb + d] + dh);
+        }
+      });
+    }
+  };
+
+  // maxima of the raw scores in s, raised where a weight would pass 2^24 (or at once)
+  auto raise = [&](const floatx4 (&s)[4][RB], bool at_once) {
+    float lm[RB];
+    bool over = at_once;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      lm[rb] = s[0][rb][0];
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lm[rb] = fmaxf(lm[rb], s[kb][rb][i]);
+      over = over || fmaf(lm[rb], sl2, -m[rb]) > kHeadroom;
+    }
+    if (__ballot(over) == 0ull) return;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const float top = wave_max_across_groups(lm[rb]) * sl2;
+      const float mnew = at_once ? top : fmaxf(m[rb], top);
+      const float f = at_once ? 0.f : fast_exp2(m[rb] - mnew);   // O and l are 0 at the start
+      l[rb] *= f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[rb][db] *= f;
+      m[rb] = mnew;
+    }
+  };
+
+  // One step, tile x of the segment: NEXT: there is a tile x + 1 in it; MASK: a
+  // row's last visible key may lie in tile x (first key t0).  PH: ring phase of
+  // x where known (the slots then sit in the instructions' offsets), else -1.
+  auto step = [&](int n, int t0, auto ph_tag, auto next_tag, auto mask_tag) {
+    constexpr int PH = decltype(ph_tag)::value;
+    constexpr bool NEXT = decltype(next_tag)::value, MASK = decltype(mask_tag)::value;
+    constexpr int PN0 = PH >= 0 ? (PH + 1) % NBUF : 0, PH0 = PH >= 0 ? PH : 0;
+    const uint32_t dn = PH >= 0 ? 0u : (uint32_t)((n + 1) % NBUF) * HALF, dh = PH >= 0 ? 0u : (uint32_t)(n % NBUF) * HALF;
+    constexpr int G0 = NEXT ? 0 : NQK;         // the last tile has no scores to form
+    bf16x8 ph[2][RB], pl[2][RB];
+    floatx4 sn[4][RB];
+    auto weights = [&](int kb) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[i] = fast_exp2(fmaf(sc[kb][rb][i], sl2, -m[rb]));
+          if constexpr (MASK) {
+            if (t0 + kb * 16 + 4 * G4 + i > lim[rb]) p[i] = 0.f;
+          }
+          const __bf16 hi = float_to_bf16(p[i]);
+          ph[kb >> 1][rb][(kb & 1) * 4 + i] = hi;
+          if constexpr (HILO) pl[kb >> 1][rb][(kb & 1) * 4 + i] = float_to_bf16(p[i] - bf16_to_float(hi));
+        }
+        l[rb] += (p[0] + p[1]) + (p[2] + p[3]);
+      }
+    };
+    reads(Const<G0>{}, Const<PN0>{}, Const<PH0>{}, dn, dh, Const<0>{});
+    if constexpr (!NEXT) {
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb) weights(kb);
+    }
+    unrolled<G0, NG>([&](auto gtag) {
+      constexpr int gr = decltype(gtag)::value;
+      reads(Const<gr + 1>{}, Const<PN0>{}, Const<PH0>{}, dn, dh, Const<0>{});
+      lds_wait_n<(gr + 1 < NQK ? 4 : gr + 1 < NG ? 8 : 0)>();
+      reads(gtag, Const<PN0>{}, Const<PH0>{}, dn, dh, Const<1>{});
+      if constexpr (gr < NQK) {
+#pragma unroll
+        for (int kk = 0; kk < KPG; ++kk) {
+          const int kb = gr * KPG + kk;
+#pragma unroll
+          for (int dc = 0; dc < DC; ++dc) {
+            Pack8 pk;
+            pk.u = xr[gr & 1][kk * DC + dc];
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+              sn[kb][rb] = mfma_bf16(pk.b, qf[rb][dc], dc == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : sn[kb][rb]);
+          }
+          weights(kb);
+        }
+        alternate<gr + 1, 4 * RB, HILO ? 6 : 3>();
+      } else {
+        constexpr int q = gr - NQK, hf = q / NPVH, pb = q % NPVH;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          Pack8 vv;
+          vv.u = u32x4{vr[gr & 1][d][0][0], vr[gr & 1][d][0][1], vr[gr & 1][d][1][0], vr[gr & 1][d][1][1]};
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb) {
+            o[rb][4 * pb + d] = mfma_bf16(vv.b, ph[hf][rb], o[rb][4 * pb + d]);
+            if constexpr (HILO) o[rb][4 * pb + d] = mfma_bf16(vv.b, pl[hf][rb], o[rb][4 * pb + d]);
+          }
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if constexpr (NEXT) {
+      raise(sn, false);
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) sc[kb][rb] = sn[kb][rb];
+    }
+  };
+
+  // Ring: entering the step of tile n the copies of tiles n + 1 and n + 2 are
+  // under way; the wait leaves tile n + 2's, the barrier frees tile n - 1's slot
+  // for tile n + 3.  Past the range the last tile is copied again.
+  Cursor ic = cc;
+  place(ic);
+  auto copy_next = [&](int slot) {
+    issue(slot);
+    if (place_behind(ic) < n1) {
+      advance<ROWS, TK>(a, ic);
+      place(ic);
+    }
+  };
+#pragma unroll 1
+  for (int i = 0; i < NBUF - 1; ++i) copy_next(i);
+  wait_vm_then_barrier<2 * 2 * COPIES>();      // tile n0 is there
+  auto begin = [&](int x) {                    // step x of the ring
+    wait_vm_then_barrier<2 * COPIES>();
+    copy_next((x + NBUF - 1) % NBUF);
+  };
+
+  int x = 0;                                   // ring step
+  while (true) {
+    const bool own = cc.u >= a.G;
+    const int rt = cc.rt, rows = cc.rows, pair = cc.pair;
+    const int steps = min(cc.nt - cc.t, n1 - cc.n);
+    const int t_first = cc.t * TK;
+    // tiles before the first with masked keys, and before the last
+    const int unmasked = own ? cc.L - a.k : cc.L - 1;
+    const int plain = max(0, min(steps - 1, (unmasked + 1) / TK - cc.t));
+    const int r0 = rt * ROWS + w * RB * 16;
+    if (r0 < rows) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const int r = r0 + rb * 16 + c;
+        Pack8 pk;
+        pk.u = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int dc = 0; dc < DC; ++dc) qf[rb][dc] = pk.b;
+        lim[rb] = -1;
+        if (r < rows) {
+          const u32x4* src = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q) +
+                                                            (size_t)out_row(a, cc.first, cc.hk, r) * D);
+#pragma unroll
+          for (int dc = 0; dc < DC; ++dc) {
+            pk.u = src[dc * 4 + G4];
+            if (neg) pk.u ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
+            qf[rb][dc] = pk.b;
+          }
+          lim[rb] = own ? cc.L - a.k + (r % kg) / g : cc.L - 1;
+        }
+        l[rb] = 0.f;
+        m[rb] = 0.f;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[rb][db] = floatx4{0.f, 0.f, 0.f, 0.f};
+      }
+      __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));   // vmcnt(0): the counted waits only see copies
+      // scores of the first tile
+      const uint32_t d0 = (uint32_t)(x % NBUF) * HALF;
+      unrolled<0, NQK>([&](auto gtag) {
+        constexpr int gr = decltype(gtag)::value;
+        reads(gtag, Const<0>{}, Const<0>{}, d0, 0u, Const<0>{});
+        lds_wait();
+        reads(gtag, Const<0>{}, Const<0>{}, d0, 0u, Const<1>{});
+#pragma unroll
+        for (int kk = 0; kk < KPG; ++kk)
+#pragma unroll
+          for (int dc = 0; dc < DC; ++dc) {
+            Pack8 pk;
+            pk.u = xr[gr & 1][kk * DC + dc];
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+              sc[gr * KPG + kk][rb] =
+                  mfma_bf16(pk.b, qf[rb][dc], dc == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : sc[gr * KPG + kk][rb]);
+          }
+      });
+      raise(sc, true);
+      int i = 0;                               // step of the segment
+#define SD_STEP(PH, NEXT, MASK)                                                                 \
+  {                                                                                             \
+    begin(x);                                                                                   \
+    step(x, t_first + i * TK, Const<PH>{}, Const<NEXT>{}, Const<MASK>{});                       \
+    ++x;                                                                                        \
+    ++i;                                                                                        \
+  }
+      while (i < plain && x % NBUF != 0) SD_STEP(-1, 1, 0)
+      while (i + NBUF <= plain) {
+        SD_STEP(0, 1, 0)
+        SD_STEP(1, 1, 0)
+        SD_STEP(2, 1, 0)
+        SD_STEP(3, 1, 0)
+      }
+      while (i < plain) SD_STEP(-1, 1, 0)
+      while (i < steps - 1) SD_STEP(-1, 1, 1)
+      SD_STEP(-1, 0, 1)
+#undef SD_STEP
+      // the segment's partial
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const float lsum = wave_sum_across_groups(l[rb]);
+        const int lr = (w * RB + rb) * 16 + c;
+        if (rt * ROWS + lr >= rows) continue;
+        const size_t prow = part_row<ROWS>(a, own, pair, wg) + lr;
+        const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+          *reinterpret_cast<floatx4*>(a.part_o + prow * D + db * 16 + 4 * G4) = o[rb][db] * inv;
+        if (G4 == 0) a.part_lse[prow] = lsum > 0.f ? m[rb] + log2f(lsum) : -INFINITY;
+      }
+    } else {
+      for (int i = 0; i < steps; ++i) begin(x++);   // no rows: its copies only
+    }
+    cc.t += steps - 1;
+    cc.n += steps - 1;
+    if (place_behind(cc) >= n1) break;
+    advance<ROWS, TK>(a, cc);
+  }
+  __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));   // no copy may still write this LDS
 }
 
 // ------------------------------------------------------------- fp32 stream
@@ -503,20 +902,21 @@ __global__ __launch_bounds__(NW * 64, 2) void shared_stream_bf16(SharedArgs a, i
 constexpr int kRowsF32 = 16;
 template <int D>
 __global__ __launch_bounds__(256) void shared_stream_f32(SharedArgs a, int G) {
-  constexpr int TK = kTile, R = kRowsF32, DS = D + 1;
+  constexpr int TK = kTileNarrow, R = kRowsF32, DS = D + 1;
   constexpr int PER = R * D / 256;             // elements of O per thread
   __shared__ float qs[R * DS], ks[TK * DS], vs[TK * DS];
   __shared__ double ps[R][TK + 1], st[R][3];   // scores / weights; max, sum, factor
   const int tid = threadIdx.x;
   const int wg = blockIdx.x;
-  const int T = total_tiles<R>(a);
+  const int T = list_length<R, TK>(a);
   const int n0 = (int)((long long)T * wg / G), n1 = (int)((long long)T * (wg + 1) / G);
   if (n0 >= n1) return;
-  Cursor cu = locate<R>(a, n0);
+  Cursor cu = locate<R, TK>(a, n0);
+  if (cu.n >= n1) return;
   const int kg = a.k * (a.Hq / a.Hkv);
   double o[PER];
   bool fresh = true;
-  for (int n = n0; n < n1; ++n) {
+  while (true) {
     const bool own = cu.u >= a.G;
     const int t0 = cu.t * TK, here = min(TK, cu.L - t0);
     __syncthreads();
@@ -589,7 +989,8 @@ __global__ __launch_bounds__(256) void shared_stream_f32(SharedArgs a, int G) {
       o[e] = acc;
     }
     fresh = cu.t + 1 == cu.nt;
-    if (fresh || n + 1 == n1) {
+    const bool end = place_behind(cu) >= n1;
+    if (fresh || end) {
       const size_t base = part_row<R>(a, own, cu.pair, wg);
 #pragma unroll
       for (int e = 0; e < PER; ++e) {
@@ -600,18 +1001,19 @@ __global__ __launch_bounds__(256) void shared_stream_f32(SharedArgs a, int G) {
         a.part_lse[base + tid] =
             st[tid][1] > 0.0 ? (float)((st[tid][0] + log(st[tid][1])) * 1.4426950408889634) : -INFINITY;
     }
-    if (n + 1 < n1) advance<R>(a, cu);
+    if (end) break;
+    advance<R, TK>(a, cu);
   }
 }
 
 // ------------------------------------------------------------------ merge
-// One wave per output row.  The tiles [U, U + nt) of a pair lie with work-groups
+// One wave per output row.  The tiles at places [U, U + nt) lie with work-groups
 // owner(U) .. owner(U + nt - 1), owner(n) = floor(((n + 1) G - 1) / T), each of
-// which wrote one partial (with fewer tiles than work-groups, each owner did).  Candidates of the prefix pair, then of the own pair,
+// which wrote one partial (with fewer places than work-groups, each owner did).  Candidates of the prefix pair, then of the own pair,
 // are taken 32 at a time: lanes 0..31 load their lse while each half-wave loads
 // the outputs of 16 of them (4 channels per lane), and the chunk's weights
 // 2^(lse - max) rescale a running sum.  Every shuffle runs on all lanes.
-template <int ROWS>
+template <int ROWS, int TK>
 __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G) {
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const long long orow = (long long)blockIdx.x * 4 + w;
@@ -622,11 +1024,11 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G) {
   const int hk = h / g;
   const int r_own = (bj - b * a.k) * g + (h - hk * g);
 
-  // tiles before, key tiles, pair and row of the prefix pair and of the own pair
+  // first tile's place, key tiles, pair and row of the prefix pair and of the own pair
   int U[2] = {0, 0}, nt[2] = {0, 0}, pair[2] = {0, 0}, lr[2] = {0, 0};
   Carry c;
   for (int u0 = 0; u0 < a.G + a.B; u0 += 64) {
-    const Span s = scan_units<ROWS>(a, u0, c);
+    const Span s = scan_units<ROWS, TK>(a, u0, c);
     const int u = u0 + lane;
     const bool is_group = u < a.G && s.un.first <= b && b < s.un.end;
 #pragma unroll
@@ -638,15 +1040,15 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G) {
       const int rows = of(s.un.rows), RT = row_tiles(rows, ROWS);
       const int r = kind == 0 ? (b - of(s.un.first)) * a.k * g + r_own : r_own;
       const int x = hk * RT + r / ROWS;
-      nt[kind] = tiles_of(of(s.un.L));
-      U[kind] = of(s.t_before) + x * nt[kind];
+      nt[kind] = tiles_of<TK>(of(s.un.L));
+      U[kind] = of(s.n_before) + x * (nt[kind] + kStart) + kStart;
       pair[kind] = kind == 0 ? of(s.p_before) + x : b * a.Hkv * RT + x;
       lr[kind] = r - r / ROWS * ROWS;
     }
   }
-  const int T = c.tiles;
+  const int T = c.places;
   auto owner = [&](int n) { return (int)((((long long)n + 1) * G - 1) / T); };
-  const bool sparse = T < G;   // then a work-group has one tile or none: a candidate per tile
+  const bool sparse = T < G;   // then a work-group has one place or none: a candidate per tile
   int wf[2] = {0, 0}, nc[2] = {0, 0};
 #pragma unroll
   for (int kind = 0; kind < 2; ++kind) {
@@ -719,10 +1121,19 @@ hipError_t launch_bf16(const SharedArgs& a, const SharedPlan& p, hipStream_t st)
   return hipGetLastError();
 }
 
-template <int ROWS>
+template <int D, int RB>
+hipError_t launch_wide(const SharedArgs& a, const SharedPlan& p, hipStream_t st) {
+  if (a.out_bf16)
+    hipLaunchKernelGGL((shared_wide_bf16<D, RB, false>), dim3(p.wgs), dim3(512), 0, st, a, p.wgs);
+  else
+    hipLaunchKernelGGL((shared_wide_bf16<D, RB, true>), dim3(p.wgs), dim3(512), 0, st, a, p.wgs);
+  return hipGetLastError();
+}
+
+template <int ROWS, int TK>
 hipError_t launch_merge(const SharedArgs& a, const SharedPlan& p, hipStream_t st) {
   const long long rows = (long long)a.B * a.k * a.Hq;
-  hipLaunchKernelGGL(shared_merge<ROWS>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a, p.wgs);
+  hipLaunchKernelGGL((shared_merge<ROWS, TK>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a, p.wgs);
   return hipGetLastError();
 }
 
@@ -748,10 +1159,11 @@ SharedPlan plan_shared(int B, int k, int Hq, int Hkv, int D, int G, int prefix_c
   const int own_tiles = (kg + p.rows_wg - 1) / p.rows_wg;
   const long long prefix_pairs = Hkv * (rows / p.rows_wg + G);
   const long long own_pairs = (long long)B * Hkv * own_tiles;
-  const long long tiles = prefix_pairs * ((prefix_cap + kTile - 1) / kTile) +
-                          own_pairs * ((cap + kTile - 1) / kTile);
-  p.ok = tiles < (1LL << 30);
-  p.wgs = (int)std::max(1LL, std::min((long long)cus * per_cu, tiles / 4));
+  const int tk = p.rows_wg == 256 ? kTileWide : kTileNarrow;
+  const long long prefix_tiles = prefix_pairs * ((prefix_cap + tk - 1) / tk);
+  const long long own_tiles_cap = own_pairs * ((cap + tk - 1) / tk);
+  p.ok = prefix_tiles + own_tiles_cap + kStart * (prefix_pairs + own_pairs) < (1LL << 30);
+  p.wgs = (int)std::max(1LL, std::min((long long)cus * per_cu, (prefix_tiles + own_tiles_cap) / 4));
   p.own_base = (prefix_pairs + p.wgs) * p.rows_wg;
   p.part_rows = (size_t)p.own_base + (size_t)(own_pairs + p.wgs) * p.rows_own;
   p.workspace_bytes = p.part_rows * ((size_t)D + 1) * sizeof(float);
@@ -766,18 +1178,18 @@ hipError_t launch_shared(const SharedArgs& a, const SharedPlan& p, int dtype, hi
     else
       hipLaunchKernelGGL(shared_stream_f32<64>, dim3(p.wgs), dim3(256), 0, st, a, p.wgs);
     e = hipGetLastError();
-    return e != hipSuccess ? e : launch_merge<kRowsF32>(a, p, st);
+    return e != hipSuccess ? e : launch_merge<kRowsF32, kTileNarrow>(a, p, st);
   }
   if (p.rows_wg == 64) {
     e = a.D == 128 ? launch_bf16<128, 4, 1, 4>(a, p, st) : launch_bf16<64, 4, 1, 8>(a, p, st);
-    return e != hipSuccess ? e : launch_merge<64>(a, p, st);
+    return e != hipSuccess ? e : launch_merge<64, kTileNarrow>(a, p, st);
   }
   if (p.rows_wg == 128) {
     e = a.D == 128 ? launch_bf16<128, 4, 2, 4>(a, p, st) : launch_bf16<64, 4, 2, 8>(a, p, st);
-    return e != hipSuccess ? e : launch_merge<128>(a, p, st);
+    return e != hipSuccess ? e : launch_merge<128, kTileNarrow>(a, p, st);
   }
-  e = a.D == 128 ? launch_bf16<128, 8, 2, 8>(a, p, st) : launch_bf16<64, 8, 2, 8>(a, p, st);
-  return e != hipSuccess ? e : launch_merge<256>(a, p, st);
+  e = a.D == 128 ? launch_wide<128, 2>(a, p, st) : launch_wide<64, 2>(a, p, st);
+  return e != hipSuccess ? e : launch_merge<256, kTileWide>(a, p, st);
 }
 
 }  // namespace sd
