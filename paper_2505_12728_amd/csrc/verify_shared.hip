@@ -40,10 +40,12 @@ namespace {
 
 
 constexpr int kTileNarrow = 32, kTileWide = 64;   // keys per tile
-// Places of the list in front of a pair's first tile: starting a pair (its
-// queries' latency with the ring drained, the partial of the one before) takes
-// about as long as this many tiles.
-constexpr int kStart = 2;
+// Places of the list in front of a pair's first tile: on the matrix cores
+// starting a pair (its queries' latency with the ring drained, the partial of
+// the one before) takes about as long as two tiles.
+constexpr int kRowsF32 = 16;
+constexpr int start_places(int rows_wg) { return rows_wg == kRowsF32 ? 0 : 2; }
+constexpr int kMergeWaves = 4096;   // rows of a sequence share a wave beyond that many
 constexpr float kHeadroom = 24.f;   // log2 of the largest weight before the maximum is raised
 
 typedef __attribute__((address_space(3))) void lds_void;
@@ -125,7 +127,7 @@ __device__ __forceinline__ Span scan_units(const SharedArgs& a, int u0, Carry& c
   }
   c.bound = max(c.bound, __shfl(bound, 63, 64));
   s.pairs = a.Hkv * row_tiles(s.un.rows, ROWS);
-  s.places = s.un.L > 0 ? s.pairs * (tiles_of<TK>(s.un.L) + kStart) : 0;
+  s.places = s.un.L > 0 ? s.pairs * (tiles_of<TK>(s.un.L) + start_places(ROWS)) : 0;
   int ti = s.places, pi = s.pairs;
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) {
@@ -168,6 +170,7 @@ __device__ __forceinline__ Cursor find_tile(const SharedArgs& a, int n) {
     cu.end = of(s.un.end);
     cu.nt = tiles_of<TK>(cu.L);
     cu.RT = row_tiles(cu.rows, ROWS);
+    constexpr int kStart = start_places(ROWS);
     const int rem = n - of(s.n_before);
     const int x = rem / (cu.nt + kStart);
     cu.t = max(rem - x * (cu.nt + kStart) - kStart, 0);
@@ -192,8 +195,9 @@ __device__ __forceinline__ Cursor locate(const SharedArgs& a, int n) {
 }
 
 // place of the tile behind cu
+template <int ROWS>
 __device__ __forceinline__ int place_behind(const Cursor& cu) {
-  return cu.n + 1 + (cu.t + 1 == cu.nt ? kStart : 0);
+  return cu.n + 1 + (cu.t + 1 == cu.nt ? start_places(ROWS) : 0);
 }
 
 // next tile of the list; the caller never steps past the last one
@@ -202,7 +206,7 @@ __device__ __forceinline__ void advance(const SharedArgs& a, Cursor& cu) {
   ++cu.n;
   if (++cu.t < cu.nt) return;
   cu.t = 0;
-  cu.n += kStart;
+  cu.n += start_places(ROWS);
   ++cu.pair;
   if (++cu.rt < cu.RT) return;
   cu.rt = 0;
@@ -241,279 +245,6 @@ __device__ __forceinline__ int out_row(const SharedArgs& a, int first, int hk, i
   const int g = a.Hq / a.Hkv;
   const int q = r / g;
   return (first * a.k + q) * a.Hq + hk * g + (r - q * g);
-}
-
-// ------------------------------------------------------------ bf16 stream
-template <int D, int NW, int RB, int NBUF, bool HILO>
-__global__ __launch_bounds__(NW * 64, 2) void shared_stream_bf16(SharedArgs a, int G) {
-  constexpr int TK = kTileNarrow;
-  constexpr int DC = D / 32;                   // 32-channel slices (S^T = K Q^T)
-  constexpr int DB = D / 16;                   // 16-channel blocks (O^T)
-  constexpr int PK = D / 8;                    // 16-byte pieces per key row
-  constexpr int ROW_BYTES = D * 2;
-  constexpr int HALF_BYTES = TK * ROW_BYTES;   // K (or V) part of a slot
-  constexpr int BUF_BYTES = 2 * HALF_BYTES;
-  constexpr int DMA_PER_HALF = TK * PK / 64;
-  constexpr int DMA_PER_WAVE = 2 * DMA_PER_HALF / NW;
-  constexpr int ROWS = NW * RB * 16;
-  static_assert((2 * DMA_PER_HALF) % NW == 0, "tile copy must split evenly");
-  static_assert(NBUF >= 3 && (NBUF - 2) * DMA_PER_WAVE < 64, "ring depth and vmcnt range");
-  __shared__ __align__(16) unsigned char ring[NBUF][BUF_BYTES];
-
-  const int lane = threadIdx.x & 63, G4 = lane >> 4, c = lane & 15;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wg = blockIdx.x;
-  const int T = __builtin_amdgcn_readfirstlane(list_length<ROWS, TK>(a));
-  const int n0 = (int)((long long)T * wg / G), n1 = (int)((long long)T * (wg + 1) / G);
-  if (n0 >= n1) return;
-  Cursor cc = locate<ROWS, TK>(a, n0);
-  if (cc.n >= n1) return;
-
-  // copies: copy i of this wave covers pieces P of K or V: key P / PK, LDS slot
-  // P % PK holding global piece slot ^ lds_swizzle(key)
-  int ckey[DMA_PER_WAVE], cpiece[DMA_PER_WAVE];
-#pragma unroll
-  for (int i = 0; i < DMA_PER_WAVE; ++i) {
-    const int P = ((w * DMA_PER_WAVE + i) % DMA_PER_HALF) * 64 + lane;
-    ckey[i] = P / PK;
-    cpiece[i] = ((P % PK) ^ lds_swizzle<PK>(P / PK)) * 8;
-  }
-  // copies of the tile under cursor cu; keys past the unit's length re-read its
-  // last key (masked)
-  auto issue = [&](const Cursor& cu, unsigned char* slot) {
-    const bool own = cu.u >= a.G;
-    const int row = own ? cu.first : cu.u;     // row of the tables and contiguous caches
-    const uint16_t* kb = static_cast<const uint16_t*>(own ? a.k_cache : a.k_prefix);
-    const uint16_t* vb = static_cast<const uint16_t*>(own ? a.v_cache : a.v_prefix);
-    const int32_t* table = own ? a.page_table : a.prefix_table;
-    const int t0 = cu.t * TK;
-    const int lim = cu.L - 1 - t0;             // last key of the tile that is there
-    if (table != nullptr) {
-      const int pages = own ? a.num_pages : a.prefix_num_pages;
-      cint32* pt = (cint32*)(table + (size_t)row * (own ? a.max_pages : a.prefix_pages));
-      const int lastp = (cu.L - 1) >> 4;
-      const int pg0 = min(max((int)pt[min(t0 >> 4, lastp)], 0), pages - 1);
-      const int pg1 = min(max((int)pt[min((t0 >> 4) + 1, lastp)], 0), pages - 1);
-      const size_t b0 = ((size_t)pg0 * a.Hkv + cu.hk) * 16 * D, b1 = ((size_t)pg1 * a.Hkv + cu.hk) * 16 * D;
-#pragma unroll
-      for (int i = 0; i < DMA_PER_WAVE; ++i) {
-        const int ii = w * DMA_PER_WAVE + i;
-        const int key = min(ckey[i], lim);
-        const size_t off = (key >> 4 ? b1 : b0) + (uint32_t)((key & 15) * D + cpiece[i]);
-        __builtin_amdgcn_global_load_lds((gbl_cvoid*)((ii / DMA_PER_HALF ? vb : kb) + off),
-                                         (lds_void*)(slot + (ii / DMA_PER_HALF) * HALF_BYTES + (ii % DMA_PER_HALF) * 1024),
-                                         16, 0, 0);
-      }
-    } else {
-      const size_t base = (((size_t)row * (own ? a.Lmax : a.prefix_cap) + t0) * a.Hkv + cu.hk) * D;
-#pragma unroll
-      for (int i = 0; i < DMA_PER_WAVE; ++i) {
-        const int ii = w * DMA_PER_WAVE + i;
-        const size_t off = base + (uint32_t)(min(ckey[i], lim) * a.Hkv * D + cpiece[i]);
-        __builtin_amdgcn_global_load_lds((gbl_cvoid*)((ii / DMA_PER_HALF ? vb : kb) + off),
-                                         (lds_void*)(slot + (ii / DMA_PER_HALF) * HALF_BYTES + (ii % DMA_PER_HALF) * 1024),
-                                         16, 0, 0);
-      }
-    }
-  };
-
-  // fragment offsets inside a slot for the first 16 keys; the swizzle depends on
-  // key % 16 only, so the second block is an immediate offset
-  uint32_t koff[DC], voff[DB];
-#pragma unroll
-  for (int dc = 0; dc < DC; ++dc) koff[dc] = c * ROW_BYTES + (((dc * 4 + G4) ^ lds_swizzle<PK>(c)) * 16);
-#pragma unroll
-  for (int db = 0; db < DB; ++db) {
-    const int key = 4 * G4 + (c >> 2), ch = db * 16 + 4 * (c & 3);
-    voff[db] = HALF_BYTES + key * ROW_BYTES + (((ch >> 3) ^ lds_swizzle<PK>(key)) * 16) + (ch & 7) * 2;
-  }
-
-  // segment state of this wave: its rows' queries (B operand of S^T = K Q^T),
-  // last visible keys and running (max, sum, O^T).  Scores stay raw, the scale
-  // enters the exponent as exp2(S sl2 - m); a negative one is folded into the
-  // queries.
-  int cur_pair = 0, cur_rt = 0, seg_rows = 0, unmasked = 0;
-  bool cur_own = false, busy = false;          // busy: this wave has rows (uniform)
-  int lim[RB];
-  bf16x8 qf[RB][DC];
-  float m[RB], l[RB];
-  floatx4 o[RB][DB];
-  const bool neg = a.scale_log2 < 0.f;
-  const float sl2 = fabsf(a.scale_log2);
-  const int kg = a.k * (a.Hq / a.Hkv);
-
-  auto start_segment = [&](const Cursor& cu) {
-    cur_pair = cu.pair;
-    cur_own = cu.u >= a.G;
-    cur_rt = cu.rt;
-    seg_rows = cu.rows;
-    busy = cu.rt * ROWS + w * RB * 16 < cu.rows;
-    unmasked = cur_own ? cu.L - a.k : cu.L - 1;
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const int r = cu.rt * ROWS + (w * RB + rb) * 16 + c;
-      Pack8 pk;
-      pk.u = u32x4{0u, 0u, 0u, 0u};
-#pragma unroll
-      for (int dc = 0; dc < DC; ++dc) qf[rb][dc] = pk.b;
-      lim[rb] = -1;
-      if (r < cu.rows) {
-        const u32x4* src = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q) +
-                                                          (size_t)out_row(a, cu.first, cu.hk, r) * D);
-#pragma unroll
-        for (int dc = 0; dc < DC; ++dc) {
-          pk.u = src[dc * 4 + G4];
-          if (neg) pk.u ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
-          qf[rb][dc] = pk.b;
-        }
-        lim[rb] = cur_own ? cu.L - a.k + (r % kg) / (kg / a.k) : cu.L - 1;
-      }
-      m[rb] = -INFINITY;
-      l[rb] = 0.f;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) o[rb][db] = floatx4{0.f, 0.f, 0.f, 0.f};
-    }
-  };
-  auto flush = [&]() {
-    if (!busy) return;
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const float lsum = wave_sum_across_groups(l[rb]);
-      const int lr = (w * RB + rb) * 16 + c;
-      if (cur_rt * ROWS + lr >= seg_rows) continue;
-      const size_t prow = part_row<ROWS>(a, cur_own, cur_pair, wg) + lr;
-      const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-        *reinterpret_cast<floatx4*>(a.part_o + prow * D + db * 16 + 4 * G4) = o[rb][db] * inv;
-      if (G4 == 0) a.part_lse[prow] = lsum > 0.f ? m[rb] + log2f(lsum) : -INFINITY;
-    }
-  };
-
-  auto compute = [&](int t0, const unsigned char* slot) {
-    const uint32_t sb = lds_addr(slot);
-    u32x4 kr[2][DC];
-#pragma unroll
-    for (int dc = 0; dc < DC; ++dc) {
-      kr[0][dc] = lds_read_b128_off<0>(sb + koff[dc]);
-      kr[1][dc] = lds_read_b128_off<16 * ROW_BYTES>(sb + koff[dc]);
-    }
-    lds_wait();
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int dc = 0; dc < DC; ++dc) tie(kr[kb][dc]);
-    u32x2 vr[2][DB];
-#pragma unroll
-    for (int db = 0; db < DB; ++db) {
-      vr[0][db] = lds_read_tr16_b64_off<0>(sb + voff[db]);
-      vr[1][db] = lds_read_tr16_b64_off<16 * ROW_BYTES>(sb + voff[db]);
-    }
-    // S^T = K Q^T: lane holds S[row c][key t0 + kb * 16 + 4 G4 + i]
-    float x[RB][8];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      floatx4 acc[RB];
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) acc[rb] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int dc = 0; dc < DC; ++dc) {
-        Pack8 pk;
-        pk.u = kr[kb][dc];
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) acc[rb] = mfma_bf16(pk.b, qf[rb][dc], acc[rb]);
-      }
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[rb][kb * 4 + i] = acc[rb][i];
-    }
-    bf16x8 ph[RB], pl[RB];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      // Exponents before the mask: their largest bounds the masked ones, so
-      // that m, raised only when a lane passes 2^24, may exceed the true maximum;
-      // it cancels in o = O / l and lse = m + log2 l.
-      float y[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = fmaf(x[rb][e], sl2, -m[rb]);
-      const float ly = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
-      if (__ballot(ly > kHeadroom) != 0ull) {
-        const float lm = fmaxf(fmaxf(fmaxf(x[rb][0], x[rb][1]), fmaxf(x[rb][2], x[rb][3])),
-                               fmaxf(fmaxf(x[rb][4], x[rb][5]), fmaxf(x[rb][6], x[rb][7])));
-        const float mnew = fmaxf(m[rb], wave_max_across_groups(lm) * sl2);
-        const float alpha = m[rb] == -INFINITY ? 0.f : fast_exp2(m[rb] - mnew);
-        l[rb] *= alpha;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) o[rb][db] *= alpha;
-        m[rb] = mnew;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = fmaf(x[rb][e], sl2, -m[rb]);
-      }
-      float p[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = fast_exp2(y[e]);
-      if (t0 + TK - 1 > unmasked) {            // tail tiles
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (t0 + (e >> 2) * 16 + 4 * G4 + (e & 3) > lim[rb]) p[e] = 0.f;
-      }
-      float sum = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        sum += p[e];
-        ph[rb][e] = float_to_bf16(p[e]);
-        if constexpr (HILO) pl[rb][e] = float_to_bf16(p[e] - bf16_to_float(ph[rb][e]));
-      }
-      l[rb] += sum;
-    }
-    // O^T += V^T P^T over keys {4 G4 .. + 3, 16 + 4 G4 .. + 3}, the order in
-    // which the score accumulator handed this lane its values
-    lds_wait();
-#pragma unroll
-    for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-      for (int db = 0; db < DB; ++db) tie(vr[hh][db]);
-#pragma unroll
-    for (int db = 0; db < DB; ++db) {
-      Pack8 vv;
-      vv.u = u32x4{vr[0][db][0], vr[0][db][1], vr[1][db][0], vr[1][db][1]};
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        o[rb][db] = mfma_bf16(vv.b, ph[rb], o[rb][db]);
-        if constexpr (HILO) o[rb][db] = mfma_bf16(vv.b, pl[rb], o[rb][db]);
-      }
-    }
-  };
-
-  // Every step issues one tile (past the range it re-reads the last one), so
-  // that at each wait exactly NBUF - 2 tiles' copies are newer than the step's
-  // own; the barrier also frees the previous step's slot.  A new segment drains
-  // this wave's memory counter, so that the counted waits only see copies.
-  Cursor ic = cc;
-  auto copy_next = [&](int slot) {
-    issue(ic, ring[slot]);
-    if (place_behind(ic) < n1) advance<ROWS, TK>(a, ic);
-  };
-#pragma unroll 1
-  for (int i = 0; i < NBUF - 1; ++i) copy_next(i);
-  bool fresh = true;
-#pragma unroll 1
-  for (int s = 0;; ++s) {
-    wait_vm_then_barrier<(NBUF - 2) * DMA_PER_WAVE>();
-    copy_next((s + NBUF - 1) % NBUF);
-    if (fresh) {
-      if (s != 0) flush();
-      start_segment(cc);
-      __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));   // vmcnt(0)
-    }
-    if (busy) compute(cc.t * TK, ring[s % NBUF]);
-    fresh = cc.t + 1 == cc.nt;
-    if (place_behind(cc) >= n1) break;
-    advance<ROWS, TK>(a, cc);
-  }
-  __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));   // no copy may still write this LDS
-  flush();
 }
 
 // ------------------------------------------------- bf16 stream, many rows
@@ -782,7 +513,7 @@ __global__ __launch_bounds__(512, 2) void shared_wide_bf16(SharedArgs a, int G) 
   place(ic);
   auto copy_next = [&](int slot) {
     issue(slot);
-    if (place_behind(ic) < n1) {
+    if (place_behind<ROWS>(ic) < n1) {
       advance<ROWS, TK>(a, ic);
       place(ic);
     }
@@ -888,7 +619,7 @@ __global__ __launch_bounds__(512, 2) void shared_wide_bf16(SharedArgs a, int G) 
     }
     cc.t += steps - 1;
     cc.n += steps - 1;
-    if (place_behind(cc) >= n1) break;
+    if (place_behind<ROWS>(cc) >= n1) break;
     advance<ROWS, TK>(a, cc);
   }
   __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));   // no copy may still write this LDS
@@ -899,7 +630,6 @@ __global__ __launch_bounds__(512, 2) void shared_wide_bf16(SharedArgs a, int G) 
 // The same list with 16 rows per work-group; a tile's keys and values and the
 // segment's queries are staged in LDS (rows padded by one float), thread i
 // forms two of the 16 x 32 scores, and O of the 16 x D elements.
-constexpr int kRowsF32 = 16;
 template <int D>
 __global__ __launch_bounds__(256) void shared_stream_f32(SharedArgs a, int G) {
   constexpr int TK = kTileNarrow, R = kRowsF32, DS = D + 1;
@@ -989,7 +719,7 @@ __global__ __launch_bounds__(256) void shared_stream_f32(SharedArgs a, int G) {
       o[e] = acc;
     }
     fresh = cu.t + 1 == cu.nt;
-    const bool end = place_behind(cu) >= n1;
+    const bool end = place_behind<R>(cu) >= n1;
     if (fresh || end) {
       const size_t base = part_row<R>(a, own, cu.pair, wg);
 #pragma unroll
@@ -1013,19 +743,19 @@ __global__ __launch_bounds__(256) void shared_stream_f32(SharedArgs a, int G) {
 // are taken 32 at a time: lanes 0..31 load their lse while each half-wave loads
 // the outputs of 16 of them (4 channels per lane), and the chunk's weights
 // 2^(lse - max) rescale a running sum.  Every shuffle runs on all lanes.
+// A wave takes `per` rows of one sequence, so that the scan over the units is
+// made once for them.
 template <int ROWS, int TK>
-__global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G) {
+__global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G, int per, int wgs_seq) {
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const long long orow = (long long)blockIdx.x * 4 + w;
-  if (orow >= (long long)a.B * a.k * a.Hq) return;
+  const int b = blockIdx.x / wgs_seq;
+  const int row0 = ((blockIdx.x - b * wgs_seq) * 4 + w) * per;   // of the k Hq rows of sequence b
+  if (row0 >= a.k * a.Hq) return;
   const int D = a.D, g = a.Hq / a.Hkv;
-  const int h = (int)(orow % a.Hq), bj = (int)(orow / a.Hq);
-  const int b = bj / a.k;
-  const int hk = h / g;
-  const int r_own = (bj - b * a.k) * g + (h - hk * g);
 
-  // first tile's place, key tiles, pair and row of the prefix pair and of the own pair
-  int U[2] = {0, 0}, nt[2] = {0, 0}, pair[2] = {0, 0}, lr[2] = {0, 0};
+  // places before the unit, key tiles, pairs before it, row tiles and first row
+  // of the sequence, for the group's prefix (0) and the sequence's own keys (1)
+  int before[2] = {0, 0}, nt[2] = {0, 0}, pairs[2] = {0, 0}, RT[2] = {1, 1}, base[2] = {0, 0};
   Carry c;
   for (int u0 = 0; u0 < a.G + a.B; u0 += 64) {
     const Span s = scan_units<ROWS, TK>(a, u0, c);
@@ -1037,21 +767,27 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G) {
       if (hit == 0ull) continue;
       const int f = __builtin_ctzll(hit);
       auto of = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
-      const int rows = of(s.un.rows), RT = row_tiles(rows, ROWS);
-      const int r = kind == 0 ? (b - of(s.un.first)) * a.k * g + r_own : r_own;
-      const int x = hk * RT + r / ROWS;
+      RT[kind] = row_tiles(of(s.un.rows), ROWS);
       nt[kind] = tiles_of<TK>(of(s.un.L));
-      U[kind] = of(s.n_before) + x * (nt[kind] + kStart) + kStart;
-      pair[kind] = kind == 0 ? of(s.p_before) + x : b * a.Hkv * RT + x;
-      lr[kind] = r - r / ROWS * ROWS;
+      before[kind] = of(s.n_before);
+      pairs[kind] = kind == 0 ? of(s.p_before) : b * a.Hkv * RT[kind];
+      base[kind] = kind == 0 ? (b - of(s.un.first)) * a.k * g : 0;
     }
   }
   const int T = c.places;
   auto owner = [&](int n) { return (int)((((long long)n + 1) * G - 1) / T); };
   const bool sparse = T < G;   // then a work-group has one place or none: a candidate per tile
-  int wf[2] = {0, 0}, nc[2] = {0, 0};
+  for (int row = row0; row < min(row0 + per, a.k * a.Hq); ++row) {
+  const int j = row / a.Hq, h = row - j * a.Hq, hk = h / g;
+  const size_t orow = (size_t)b * a.k * a.Hq + row;
+  int U[2], pair[2], lr[2], wf[2] = {0, 0}, nc[2] = {0, 0};
 #pragma unroll
   for (int kind = 0; kind < 2; ++kind) {
+    const int r = base[kind] + j * g + (h - hk * g);
+    const int x = hk * RT[kind] + r / ROWS;
+    U[kind] = before[kind] + x * (nt[kind] + start_places(ROWS)) + start_places(ROWS);
+    pair[kind] = pairs[kind] + x;
+    lr[kind] = r % ROWS;
     if (nt[kind] == 0) continue;
     wf[kind] = owner(U[kind]);
     nc[kind] = sparse ? nt[kind] : owner(U[kind] + nt[kind] - 1) - wf[kind] + 1;
@@ -1104,21 +840,13 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G) {
       Pack8 pk;
 #pragma unroll
       for (int e = 0; e < 4; ++e) pk.b[e] = float_to_bf16(v[e]);
-      *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + (size_t)orow * D + d4 * 4) = u32x2{pk.u[0], pk.u[1]};
+      *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + orow * D + d4 * 4) = u32x2{pk.u[0], pk.u[1]};
     } else {
-      *reinterpret_cast<floatx4*>(static_cast<float*>(a.out) + (size_t)orow * D + d4 * 4) = v;
+      *reinterpret_cast<floatx4*>(static_cast<float*>(a.out) + orow * D + d4 * 4) = v;
     }
   }
   if (a.lse != nullptr && lane == 0) a.lse[orow] = wsum > 0.f ? (mx + log2f(wsum)) * kLn2 : -INFINITY;
-}
-
-template <int D, int NW, int RB, int NBUF>
-hipError_t launch_bf16(const SharedArgs& a, const SharedPlan& p, hipStream_t st) {
-  if (a.out_bf16)
-    hipLaunchKernelGGL((shared_stream_bf16<D, NW, RB, NBUF, false>), dim3(p.wgs), dim3(NW * 64), 0, st, a, p.wgs);
-  else
-    hipLaunchKernelGGL((shared_stream_bf16<D, NW, RB, NBUF, true>), dim3(p.wgs), dim3(NW * 64), 0, st, a, p.wgs);
-  return hipGetLastError();
+  }
 }
 
 template <int D, int RB>
@@ -1132,8 +860,12 @@ hipError_t launch_wide(const SharedArgs& a, const SharedPlan& p, hipStream_t st)
 
 template <int ROWS, int TK>
 hipError_t launch_merge(const SharedArgs& a, const SharedPlan& p, hipStream_t st) {
-  const long long rows = (long long)a.B * a.k * a.Hq;
-  hipLaunchKernelGGL((shared_merge<ROWS, TK>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a, p.wgs);
+  // about kMergeWaves waves, a whole number of rows each
+  const int rows = a.k * a.Hq;
+  const int per = (int)std::max(1LL, std::min((long long)rows, (long long)a.B * rows / kMergeWaves));
+  const int wgs_seq = (rows + 4 * per - 1) / (4 * per);
+  hipLaunchKernelGGL((shared_merge<ROWS, TK>), dim3((unsigned)(a.B * (long long)wgs_seq)), dim3(256), 0, st, a, p.wgs, per,
+                     wgs_seq);
   return hipGetLastError();
 }
 
@@ -1152,17 +884,17 @@ SharedPlan plan_shared(int B, int k, int Hq, int Hkv, int D, int G, int prefix_c
     // rows of an average group; a wave of two 16-row blocks halves the LDS reads
     // per product, eight such waves halve the HBM reads per row again
     const long long avg = (rows + G - 1) / G;
-    p.rows_wg = avg <= 64 ? 64 : avg <= 128 ? 128 : 256;
-    per_cu = p.rows_wg == 256 ? 1 : 2;
+    p.rows_wg = avg <= 128 ? 128 : 256;
+    per_cu = 1;
   }
   p.rows_own = std::min((kg + 15) / 16 * 16, p.rows_wg);
   const int own_tiles = (kg + p.rows_wg - 1) / p.rows_wg;
   const long long prefix_pairs = Hkv * (rows / p.rows_wg + G);
   const long long own_pairs = (long long)B * Hkv * own_tiles;
-  const int tk = p.rows_wg == 256 ? kTileWide : kTileNarrow;
+  const int tk = p.rows_wg >= 128 ? kTileWide : kTileNarrow;
   const long long prefix_tiles = prefix_pairs * ((prefix_cap + tk - 1) / tk);
   const long long own_tiles_cap = own_pairs * ((cap + tk - 1) / tk);
-  p.ok = prefix_tiles + own_tiles_cap + kStart * (prefix_pairs + own_pairs) < (1LL << 30);
+  p.ok = prefix_tiles + own_tiles_cap + start_places(p.rows_wg) * (prefix_pairs + own_pairs) < (1LL << 30);
   p.wgs = (int)std::max(1LL, std::min((long long)cus * per_cu, (prefix_tiles + own_tiles_cap) / 4));
   p.own_base = (prefix_pairs + p.wgs) * p.rows_wg;
   p.part_rows = (size_t)p.own_base + (size_t)(own_pairs + p.wgs) * p.rows_own;
@@ -1180,13 +912,9 @@ hipError_t launch_shared(const SharedArgs& a, const SharedPlan& p, int dtype, hi
     e = hipGetLastError();
     return e != hipSuccess ? e : launch_merge<kRowsF32, kTileNarrow>(a, p, st);
   }
-  if (p.rows_wg == 64) {
-    e = a.D == 128 ? launch_bf16<128, 4, 1, 4>(a, p, st) : launch_bf16<64, 4, 1, 8>(a, p, st);
-    return e != hipSuccess ? e : launch_merge<64, kTileNarrow>(a, p, st);
-  }
   if (p.rows_wg == 128) {
-    e = a.D == 128 ? launch_bf16<128, 4, 2, 4>(a, p, st) : launch_bf16<64, 4, 2, 8>(a, p, st);
-    return e != hipSuccess ? e : launch_merge<128, kTileNarrow>(a, p, st);
+    e = a.D == 128 ? launch_wide<128, 1>(a, p, st) : launch_wide<64, 1>(a, p, st);
+    return e != hipSuccess ? e : launch_merge<128, kTileWide>(a, p, st);
   }
   e = a.D == 128 ? launch_wide<128, 2>(a, p, st) : launch_wide<64, 2>(a, p, st);
   return e != hipSuccess ? e : launch_merge<256, kTileWide>(a, p, st);
