@@ -185,10 +185,21 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _current(name, t):
-    """The library launches on the current device: tensors of another one are refused."""
-    if t.device.index != _torch()._C._cuda_getDevice():
-        raise ValueError(f"{name} is on {t.device}, which is not the current device")
+def _on_current(*named):
+    """The library launches on the current device: every tensor (name, tensor or
+    None) lies there.  One comparison each; the messages come afterwards."""
+    c = _torch()._C._cuda_getDevice()
+    for name, t in named:
+        if t is not None and t.get_device() != c:
+            if not t.is_cuda:
+                raise ValueError(f"{name} must be a GPU tensor")
+            raise ValueError(f"{name} must be on cuda:{c}, the current device, got {t.device}")
+
+
+def _dense(t, name, dtype, ndim):
+    if t.dtype == dtype and t.dim() == ndim and t.is_contiguous():
+        return
+    _check(t, name, dtype, ndim)
 
 
 def _pages(num_pages, pool):
@@ -807,30 +818,30 @@ def sd_avg_pool_compress(feats, C, out=None, stream=None):
 
 def _rows(t, name, dtype=None):
     """A [T, H, D] tensor whose rows are dense; they may lie any stride apart
-    (a slice of a fused projection).  Returns that stride in elements."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a GPU tensor")
+    (a slice of a fused projection).  Returns its shape and that stride in
+    elements."""
     if t.dim() != 3:
         raise ValueError(f"{name} must have 3 dimensions, got {t.dim()}")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    T, H, D = t.shape
+    shape = T, H, D = t.shape
     sT, sH, sD = t.stride()
+    if sD == 1 and sH == D and sT >= H * D:
+        return shape, sT
     if (D > 1 and sD != 1) or (H > 1 and sH != D) or (T > 1 and sT < H * D):
         raise ValueError(f"{name} must be [T, H, D] with dense rows (any stride between rows)")
-    return sT if T > 1 else H * D
+    return shape, (sT if T > 1 else H * D)
 
 
-def _axes(pos, sections, T, device):
-    """(positions as [axes, T] or None, number of axes, sections as a C array or None)."""
-    torch = _torch()
+def _axes(pos, sections, T):
+    """(number of axes, sections as a C array or None); pos [axes, T], [T] or None."""
     axes = None
     if pos is not None:
-        _check(pos, "pos", dtype=torch.int32)
-        if pos.dim() not in (1, 2) or pos.shape[-1] != T:
+        ndim = pos.dim()
+        if ndim not in (1, 2) or pos.shape[-1] != T:
             raise ValueError(f"pos must be [axes, {T}] or [{T}], got {tuple(pos.shape)}")
-        _same_device("pos", pos, device)
-        axes = pos.shape[0] if pos.dim() == 2 else 1
+        _dense(pos, "pos", _torch().int32, ndim)
+        axes = pos.shape[0] if ndim == 2 else 1
     if sections is None:
         return 1 if axes is None else axes, None
     n = len(sections)
@@ -845,19 +856,19 @@ def sd_rope(x, pos, theta, sections=None, per_axis=False, inverse=False, out=Non
     one axis, all D / 2).  per_axis restarts the frequencies in every section.
     inverse turns back, which is also the gradient: dx = sd_rope(dy, ...,
     inverse=True).  out may be x (in place).  Returns out [T, H, D]."""
-    torch = _torch()
-    xs = _rows(x, "x")
-    _current("x", x)
+    _on_current(("x", x), ("pos", pos), ("out", out))
+    shape, xs = _rows(x, "x")
+    T, H, D = shape
     dt = _dtype_code(x)
-    T, H, D = x.shape
-    axes, secs = _axes(pos, sections, T, x.device)
+    axes, secs = _axes(pos, sections, T)
     if out is None:
-        out = _empty((T, H, D), x.dtype, x.device, stream)
-    ys = _rows(out, "out", x.dtype)
-    if out.shape != x.shape:
-        raise ValueError(f"out must have shape {tuple(x.shape)}, got {tuple(out.shape)}")
-    _same_device("out", out, x.device)
-    st = library().sd_rope(_ptr(x), xs, _ptr(pos), _ptr(out), ys, T, H, D, axes, secs, float(theta),
+        out = _empty(shape, x.dtype, x.device, stream)
+        ys = H * D
+    else:
+        out_shape, ys = _rows(out, "out", x.dtype)
+        if out_shape != shape:
+            raise ValueError(f"out must have shape {tuple(shape)}, got {tuple(out_shape)}")
+    st = library().sd_rope(x.data_ptr(), xs, pos.data_ptr(), out.data_ptr(), ys, T, H, D, axes, secs, theta,
                            SD_ROPE_PER_AXIS if per_axis else SD_ROPE_RUNNING, 1 if inverse else 0, dt,
                            _stream(stream))
     _raise(st, "sd_rope")
@@ -875,55 +886,59 @@ def sd_kv_append(q, k, v, k_cache, v_cache, kv_len, theta, pos=None, sections=No
     all), see sd_rope.  fp32 rows may go into a bf16 cache.  The caches are
     written in place.  Returns the rotated queries [T, Hq, D] in the cache's
     dtype (None without q)."""
-    torch = _torch()
-    ks, vs = _rows(k, "k"), _rows(v, "v", k.dtype)
-    _current("k", k)
-    _check(k_cache, "k_cache", ndim=4)
-    _check(v_cache, "v_cache", dtype=k_cache.dtype, ndim=4)
-    _check(kv_len, "kv_len", dtype=torch.int32, ndim=1)
-    T, Hkv, D = k.shape
+    int32 = _torch().int32
+    _on_current(("q", q), ("k", k), ("v", v), ("k_cache", k_cache), ("v_cache", v_cache), ("kv_len", kv_len),
+                ("pos", pos), ("row_start", row_start), ("page_table", page_table), ("q_out", q_out))
+    src, dtype = k.dtype, k_cache.dtype
+    shape, ks = _rows(k, "k")
+    v_shape, vs = _rows(v, "v", src)
+    T, Hkv, D = shape
+    _dense(k_cache, "k_cache", dtype, 4)
+    _dense(v_cache, "v_cache", dtype, 4)
+    _dense(kv_len, "kv_len", int32, 1)
     B = kv_len.shape[0]
-    if v.shape != k.shape:
+    cache = k_cache.shape
+    if v_shape != shape:
         raise ValueError("k and v must have the same shape")
-    if k_cache.shape != v_cache.shape:
+    if cache != v_cache.shape:
         raise ValueError("k_cache and v_cache must have the same shape")
-    dev = k.device
     if page_table is None:
-        if k_cache.shape[0] != B or k_cache.shape[2] != Hkv or k_cache.shape[3] != D:
+        if cache[0] != B or cache[2] != Hkv or cache[3] != D:
             raise ValueError("contiguous caches must be [B, Lmax, Hkv, D]")
-        Lmax, max_pages, num_pages_ = k_cache.shape[1], 0, 0
+        table, Lmax, max_pages, pages = None, cache[1], 0, 0
     else:
-        _check(page_table, "page_table", dtype=torch.int32, ndim=2)
-        if (k_cache.shape[1] != Hkv or k_cache.shape[2] != 16 or k_cache.shape[3] != D
-                or page_table.shape[0] != B):
+        _dense(page_table, "page_table", int32, 2)
+        if cache[1] != Hkv or cache[2] != 16 or cache[3] != D or page_table.shape[0] != B:
             raise ValueError("paged caches must be [P, Hkv, 16, D] with a [B, max_pages] table")
-        Lmax, max_pages = 0, page_table.shape[1]
-        num_pages_ = _pages(num_pages, k_cache)
+        table, Lmax, max_pages, pages = page_table.data_ptr(), 0, page_table.shape[1], _pages(num_pages, k_cache)
     if row_start is not None:
-        _check(row_start, "row_start", dtype=torch.int32, ndim=1)
+        _dense(row_start, "row_start", int32, 1)
         if row_start.shape[0] != B + 1:
             raise ValueError("row_start must be [B + 1]")
+        row_start = row_start.data_ptr()
     elif T % B != 0:
         raise ValueError("without row_start every sequence has T / B rows")
-    Hq, qs = 0, 0
+    Hq = qs = 0
+    qp = qop = None
     if q is not None:
-        qs = _rows(q, "q", k.dtype)
-        Hq = q.shape[1]
-        if q.shape[0] != T or q.shape[2] != D:
+        q_shape, qs = _rows(q, "q", src)
+        Hq = q_shape[1]
+        if q_shape[0] != T or q_shape[2] != D:
             raise ValueError("q must be [T, Hq, D] with the rows of k")
         if q_out is None:
-            q_out = _empty((T, Hq, D), k_cache.dtype, dev, stream)
-        _out(q_out, "q_out", (T, Hq, D), k_cache.dtype, dev)
+            q_out = _empty(q_shape, dtype, k.device, stream)
+        else:
+            _out(q_out, "q_out", (T, Hq, D), dtype, k.device)
+        qp, qop = q.data_ptr(), q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("q_out without q")
-    axes, secs = (0, None) if theta is None else _axes(pos, sections, T, dev)
-    for name, t in (("q", q), ("v", v), ("k_cache", k_cache), ("v_cache", v_cache), ("kv_len", kv_len),
-                    ("row_start", row_start), ("page_table", page_table)):
-        _same_device(name, t, dev)
-    st = library().sd_kv_append(_ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _ptr(q_out), _ptr(k_cache), _ptr(v_cache),
-                                _ptr(row_start), _ptr(kv_len), _ptr(page_table), max_pages, num_pages_, Lmax,
-                                None if theta is None else _ptr(pos), T, B, Hq, Hkv, D, axes, secs,
-                                0.0 if theta is None else float(theta),
+    axes, secs, p = 0, None, None
+    if theta is not None:
+        axes, secs = _axes(pos, sections, T)
+        p = _ptr(pos)
+    st = library().sd_kv_append(qp, qs, k.data_ptr(), ks, v.data_ptr(), vs, qop, k_cache.data_ptr(),
+                                v_cache.data_ptr(), row_start, kv_len.data_ptr(), table, max_pages, pages, Lmax, p, T,
+                                B, Hq, Hkv, D, axes, secs, theta or 0.0,
                                 SD_ROPE_PER_AXIS if per_axis else SD_ROPE_RUNNING, _dtype_code(k),
                                 _dtype_code(k_cache), _stream(stream))
     _raise(st, "sd_kv_append")
@@ -936,24 +951,24 @@ def sd_verify_shared_workspace_size(B, k, Hq, Hkv, D, G, prefix_capacity, capaci
     return library().sd_verify_shared_workspace_size(B, k, Hq, Hkv, D, G, prefix_capacity, capacity, dtype)
 
 
-def _cache_shape(k, v, rows, table, D, dtype, names, device, num_pages=None):
+def _cache_shape(k, v, rows, table, D, dtype, names, num_pages=None):
     """Checks a contiguous cache [rows, L, Hkv, D] or page pools [P, Hkv, 16,
     D] with their table [rows, pages].  Returns (Hkv, capacity, pages of the
-    table, pages of the pool, L)."""
-    _check(k, names[0], dtype=dtype, ndim=4)
-    _check(v, names[1], dtype=dtype, ndim=4)
-    if k.shape != v.shape:
+    table, pages of the pool, L, the table's address)."""
+    _dense(k, names[0], dtype, 4)
+    _dense(v, names[1], dtype, 4)
+    shape = k.shape
+    if shape != v.shape:
         raise ValueError(f"{names[0]} and {names[1]} must have the same shape")
-    for name, t in zip(names, (k, v, table)):
-        _same_device(name, t, device)
     if table is None:
-        if k.shape[0] != rows or k.shape[3] != D:
-            raise ValueError(f"contiguous {names[0]} must be [{rows}, L, Hkv, {D}], got {tuple(k.shape)}")
-        return k.shape[2], k.shape[1], 0, 0, k.shape[1]
-    _check(table, names[2], dtype=_torch().int32, ndim=2)
-    if k.shape[2] != 16 or k.shape[3] != D or table.shape[0] != rows:
+        if shape[0] != rows or shape[3] != D:
+            raise ValueError(f"contiguous {names[0]} must be [{rows}, L, Hkv, {D}], got {tuple(shape)}")
+        return shape[2], shape[1], 0, 0, shape[1], None
+    _dense(table, names[2], _torch().int32, 2)
+    if shape[2] != 16 or shape[3] != D or table.shape[0] != rows:
         raise ValueError(f"paged {names[0]} must be [P, Hkv, 16, {D}] with {names[2]} [{rows}, pages]")
-    return k.shape[1], 16 * table.shape[1], table.shape[1], _pages(num_pages, k), 0
+    pages = table.shape[1]
+    return shape[1], 16 * pages, pages, _pages(num_pages, k), 0, table.data_ptr()
 
 
 def sd_verify_shared(q, k_cache, v_cache, kv_len, prefix_len, k_prefix=None, v_prefix=None, prefix_table=None,
@@ -970,56 +985,61 @@ def sd_verify_shared(q, k_cache, v_cache, kv_len, prefix_len, k_prefix=None, v_p
     (the default) or, for bf16 inputs, bfloat16.
     Returns (out [B, k, Hq, D], lse [B, k, Hq] fp32 or None)."""
     torch = _torch()
-    _check(q, "q", ndim=4)
-    _current("q", q)
-    _check(kv_len, "kv_len", dtype=torch.int32, ndim=1)
-    _check(prefix_len, "prefix_len", dtype=torch.int32, ndim=1)
-    B, k, Hq, D = q.shape
+    int32, dtype = torch.int32, q.dtype
+    _on_current(("q", q), ("k_cache", k_cache), ("v_cache", v_cache), ("kv_len", kv_len), ("prefix_len", prefix_len),
+                ("k_prefix", k_prefix), ("v_prefix", v_prefix), ("prefix_table", prefix_table),
+                ("group_start", group_start), ("page_table", page_table))
+    _dense(q, "q", dtype, 4)
+    _dense(kv_len, "kv_len", int32, 1)
+    _dense(prefix_len, "prefix_len", int32, 1)
+    shape = B, k, Hq, D = q.shape
     G = prefix_len.shape[0]
-    dev = q.device
     if kv_len.shape[0] != B:
         raise ValueError("kv_len needs one entry per sequence")
     if (k_prefix is None) != (v_prefix is None):
         raise ValueError("k_prefix and v_prefix come together")
-    if k_prefix is None:
+    own_pool = k_prefix is None
+    if own_pool:
         if page_table is None or prefix_table is None:
             raise ValueError("without k_prefix the prefixes are pages of the caches: both tables are needed")
         k_prefix, v_prefix = k_cache, v_cache
     dt = _dtype_code(q)
-    Hkv, cap, max_pages, num_pages_, Lmax = _cache_shape(k_cache, v_cache, B, page_table, D, q.dtype,
-                                                         ("k_cache", "v_cache", "page_table"), dev, num_pages)
-    Hkv_p, pcap, ppages, pnum, pL = _cache_shape(k_prefix, v_prefix, G, prefix_table, D, q.dtype,
-                                                 ("k_prefix", "v_prefix", "prefix_table"), dev,
-                                                 num_pages if k_prefix is k_cache else None)
+    Hkv, cap, max_pages, pages, Lmax, table = _cache_shape(k_cache, v_cache, B, page_table, D, dtype,
+                                                           ("k_cache", "v_cache", "page_table"), num_pages)
+    Hkv_p, pcap, ppages, ppool, pL, ptable = _cache_shape(k_prefix, v_prefix, G, prefix_table, D, dtype,
+                                                          ("k_prefix", "v_prefix", "prefix_table"),
+                                                          num_pages if own_pool else None)
     if Hkv_p != Hkv:
         raise ValueError("prefixes and caches must have the same KV heads")
+    groups = None
     if group_start is not None:
-        _check(group_start, "group_start", dtype=torch.int32, ndim=1)
+        _dense(group_start, "group_start", int32, 1)
         if group_start.shape[0] != G + 1:
             raise ValueError("group_start must be [G + 1]")
-    for name, t in (("kv_len", kv_len), ("prefix_len", prefix_len), ("group_start", group_start)):
-        _same_device(name, t, dev)
+        groups = group_start.data_ptr()
     if scale is None:
         scale = 1.0 / math.sqrt(D)
     if out_dtype is None:
         out_dtype = torch.float32 if out is None else out.dtype
     if out_dtype != torch.float32 and out_dtype != torch.bfloat16:
         raise TypeError(f"unsupported out_dtype {out_dtype}: use float32 or bfloat16")
+    dev = q.device
     if out is None:
-        out = _empty((B, k, Hq, D), out_dtype, dev, stream)
-    _out(out, "out", (B, k, Hq, D), out_dtype, dev)
+        out = _empty(shape, out_dtype, dev, stream)
+    else:
+        _out(out, "out", shape, out_dtype, dev)
     lse_t = None
     if lse is True:
-        lse_t = _empty((B, k, Hq), torch.float32, dev, stream)
+        lse_t = _empty(shape[:3], torch.float32, dev, stream)
     elif lse is not None and lse is not False:
-        lse_t = _out(lse, "lse", (B, k, Hq), torch.float32, dev)
-    ws_bytes = sd_verify_shared_workspace_size(B, k, Hq, Hkv, D, G, pcap, cap, dt)
-    ws, ws_len = _scratch(ws_bytes, dev, workspace, stream)
-    st = library().sd_verify_shared(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(kv_len), _ptr(page_table), max_pages,
-                                    num_pages_, Lmax, _ptr(k_prefix), _ptr(v_prefix), _ptr(prefix_len),
-                                    _ptr(prefix_table), ppages, pnum, pL, _ptr(group_start), _ptr(out), _ptr(lse_t),
-                                    B, k, Hq, Hkv, D, G, float(scale), dt,
-                                    SD_F32 if out_dtype == torch.float32 else SD_BF16, _ptr(ws), ws_len,
-                                    _stream(stream))
+        lse_t = _out(lse, "lse", shape[:3], torch.float32, dev)
+    lib = library()
+    ws, ws_len = _scratch(lib.sd_verify_shared_workspace_size(B, k, Hq, Hkv, D, G, pcap, cap, dt), dev, workspace,
+                          stream)
+    st = lib.sd_verify_shared(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), kv_len.data_ptr(), table,
+                              max_pages, pages, Lmax, k_prefix.data_ptr(), v_prefix.data_ptr(), prefix_len.data_ptr(),
+                              ptable, ppages, ppool, pL, groups, out.data_ptr(), _ptr(lse_t), B, k, Hq, Hkv, D, G,
+                              scale, dt, SD_F32 if out_dtype == torch.float32 else SD_BF16, _ptr(ws), ws_len,
+                              _stream(stream))
     _raise(st, "sd_verify_shared")
     return out, lse_t

@@ -39,7 +39,7 @@ namespace sd {
 namespace {
 
 
-constexpr int kTileNarrow = 32, kTileWide = 64;   // keys per tile
+constexpr int kTileF32 = 32, kTile = 64;   // keys per tile (fp32, bf16)
 // Places of the list in front of a pair's first tile: on the matrix cores
 // starting a pair (its queries' latency with the ring drained, the partial of
 // the one before) takes about as long as two tiles.
@@ -278,7 +278,7 @@ __device__ __forceinline__ void unrolled(F&& f) {
 
 template <int D, int RB, bool HILO>
 __global__ __launch_bounds__(512, 2) void shared_wide_bf16(SharedArgs a, int G) {
-  constexpr int NW = 8, TK = kTileWide, NBUF = 4;
+  constexpr int NW = 8, TK = kTile, NBUF = 4;
   constexpr int DC = D / 32;                   // 32-channel slices (S^T = K Q^T)
   constexpr int DB = D / 16;                   // 16-channel blocks (O^T)
   constexpr int PK = D / 8;                    // 16-byte pieces per key row
@@ -627,16 +627,18 @@ __global__ __launch_bounds__(512, 2) void shared_wide_bf16(SharedArgs a, int G) 
 
 // ------------------------------------------------------------- fp32 stream
 // fp32 inputs: scores, softmax and P V in float64, as everywhere for fp32.
-// The same list with 16 rows per work-group; a tile's keys and values and the
-// segment's queries are staged in LDS (rows padded by one float), thread i
-// forms two of the 16 x 32 scores, and O of the 16 x D elements.
+// The same list with 16 rows per work-group and 32-key tiles.  The segment's
+// queries and a tile's keys and values lie in LDS (rows padded by one float);
+// row r belongs to the 16 lanes r * 16 ..: each forms two of its scores, its
+// maximum and sum go over those lanes by shuffles, and each accumulates D / 16
+// of its channels.
 template <int D>
 __global__ __launch_bounds__(256) void shared_stream_f32(SharedArgs a, int G) {
-  constexpr int TK = kTileNarrow, R = kRowsF32, DS = D + 1;
-  constexpr int PER = R * D / 256;             // elements of O per thread
+  constexpr int TK = kTileF32, R = kRowsF32, DS = D + 1;
+  constexpr int PER = D / 16;                  // channels per lane
   __shared__ float qs[R * DS], ks[TK * DS], vs[TK * DS];
-  __shared__ double ps[R][TK + 1], st[R][3];   // scores / weights; max, sum, factor
-  const int tid = threadIdx.x;
+  __shared__ double ps[R][TK + 1];             // weights
+  const int tid = threadIdx.x, r = tid >> 4, lane16 = tid & 15;
   const int wg = blockIdx.x;
   const int T = list_length<R, TK>(a);
   const int n0 = (int)((long long)T * wg / G), n1 = (int)((long long)T * (wg + 1) / G);
@@ -644,92 +646,87 @@ __global__ __launch_bounds__(256) void shared_stream_f32(SharedArgs a, int G) {
   Cursor cu = locate<R, TK>(a, n0);
   if (cu.n >= n1) return;
   const int kg = a.k * (a.Hq / a.Hkv);
-  double o[PER];
+  double o[PER], m = -INFINITY, l = 0.0;
   bool fresh = true;
   while (true) {
     const bool own = cu.u >= a.G;
     const int t0 = cu.t * TK, here = min(TK, cu.L - t0);
-    __syncthreads();
+    const int row = cu.rt * R + r;             // of the unit
+    __syncthreads();                           // the previous tile's reads are done
     if (fresh) {
       for (int i = tid; i < R * D; i += 256) {
-        const int r = cu.rt * R + i / D;
+        const int qr = cu.rt * R + i / D;
         qs[(i / D) * DS + i % D] =
-            r < cu.rows ? static_cast<const float*>(a.q)[(size_t)out_row(a, cu.first, cu.hk, r) * D + i % D] : 0.f;
+            qr < cu.rows ? static_cast<const float*>(a.q)[(size_t)out_row(a, cu.first, cu.hk, qr) * D + i % D] : 0.f;
       }
 #pragma unroll
       for (int e = 0; e < PER; ++e) o[e] = 0.0;
-      if (tid < R) {
-        st[tid][0] = -INFINITY;
-        st[tid][1] = 0.0;
-      }
+      m = -INFINITY;
+      l = 0.0;
     }
-    const int row = own ? cu.first : cu.u;
+    const int seq = own ? cu.first : cu.u;
     const float* kb = static_cast<const float*>(own ? a.k_cache : a.k_prefix);
     const float* vb = static_cast<const float*>(own ? a.v_cache : a.v_prefix);
     const int32_t* table = own ? a.page_table : a.prefix_table;
-    for (int i = tid; i < here * D; i += 256) {
-      const int t = t0 + i / D;
+#pragma unroll 4
+    for (int i = tid; i < TK * D; i += 256) {
+      const int t = min(t0 + i / D, cu.L - 1);   // past the length: the last key, masked
       size_t off;
       if (table != nullptr) {
         const int pages = own ? a.num_pages : a.prefix_num_pages;
-        const int page = min(max(table[(size_t)row * (own ? a.max_pages : a.prefix_pages) + (t >> 4)], 0), pages - 1);
+        const int page = min(max(table[(size_t)seq * (own ? a.max_pages : a.prefix_pages) + (t >> 4)], 0), pages - 1);
         off = (((size_t)page * a.Hkv + cu.hk) * 16 + (t & 15)) * D;
       } else {
-        off = (((size_t)row * (own ? a.Lmax : a.prefix_cap) + t) * a.Hkv + cu.hk) * D;
+        off = (((size_t)seq * (own ? a.Lmax : a.prefix_cap) + t) * a.Hkv + cu.hk) * D;
       }
       ks[(i / D) * DS + i % D] = kb[off + i % D];
       vs[(i / D) * DS + i % D] = vb[off + i % D];
     }
     __syncthreads();
-    for (int i = tid; i < R * TK; i += 256) {
-      const int r = i / TK, t = i % TK, gr = cu.rt * R + r;
-      const int lim = own ? cu.L - a.k + (gr % kg) / (kg / a.k) : cu.L - 1;
-      double s = -INFINITY;
-      if (gr < cu.rows && t < here && t0 + t <= lim) {
-        double acc = 0.0;
-        for (int e = 0; e < D; ++e) acc = fma((double)qs[r * DS + e], (double)ks[t * DS + e], acc);
-        s = acc * (double)a.scale;
-      }
-      ps[r][t] = s;
+    const int lim = own ? cu.L - a.k + (row % kg) / (kg / a.k) : cu.L - 1;
+    double s[2] = {0.0, 0.0};
+    for (int e = 0; e < D; ++e) {
+      const double q = (double)qs[r * DS + e];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) s[i] = fma(q, (double)ks[(lane16 + 16 * i) * DS + e], s[i]);
     }
-    __syncthreads();
-    if (tid < R) {
-      double mx = st[tid][0];
-      for (int t = 0; t < TK; ++t) mx = fmax(mx, ps[tid][t]);
-      const double f = st[tid][0] == -INFINITY ? 0.0 : exp(st[tid][0] - mx);
-      double sum = st[tid][1] * f;
-      for (int t = 0; t < TK; ++t) {
-        const double p = mx == -INFINITY ? 0.0 : exp(ps[tid][t] - mx);
-        ps[tid][t] = p;
-        sum += p;
-      }
-      st[tid][0] = mx;
-      st[tid][1] = sum;
-      st[tid][2] = f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int t = lane16 + 16 * i;
+      s[i] = t < here && t0 + t <= lim ? s[i] * (double)a.scale : -INFINITY;
     }
+    double top = fmax(s[0], s[1]);
+#pragma unroll
+    for (int off = 8; off > 0; off >>= 1) top = fmax(top, __shfl_xor(top, off, 64));
+    top = fmax(m, top);
+    const double keep = m == -INFINITY ? 0.0 : exp(m - top);
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const double p = s[i] == -INFINITY ? 0.0 : exp(s[i] - top);
+      ps[r][lane16 + 16 * i] = p;
+      sum += p;
+    }
+#pragma unroll
+    for (int off = 8; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    l = l * keep + sum;
+    m = top;
     __syncthreads();
 #pragma unroll
-    for (int e = 0; e < PER; ++e) {
-      const int i = tid + e * 256, r = i / D, ch = i % D;
-      double acc = o[e] * st[r][2];
-      for (int t = 0; t < here; ++t) {
-        const double p = ps[r][t];
-        acc = fma(p, p != 0.0 ? (double)vs[t * DS + ch] : 0.0, acc);   // a zero weight adds nothing
-      }
-      o[e] = acc;
+    for (int e = 0; e < PER; ++e) o[e] *= keep;
+    for (int t = 0; t < here; ++t) {
+      const double p = ps[r][t];
+#pragma unroll
+      for (int e = 0; e < PER; ++e)
+        o[e] = fma(p, p != 0.0 ? (double)vs[t * DS + lane16 + 16 * e] : 0.0, o[e]);   // a zero weight adds nothing
     }
     fresh = cu.t + 1 == cu.nt;
     const bool end = place_behind<R>(cu) >= n1;
-    if (fresh || end) {
-      const size_t base = part_row<R>(a, own, cu.pair, wg);
+    if ((fresh || end) && row < cu.rows) {
+      const size_t at = part_row<R>(a, own, cu.pair, wg) + r;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) {
-        const int i = tid + e * 256, r = i / D;
-        if (cu.rt * R + r < cu.rows) a.part_o[(base + r) * D + i % D] = st[r][1] > 0.0 ? (float)(o[e] / st[r][1]) : 0.f;
-      }
-      if (tid < R && cu.rt * R + tid < cu.rows)
-        a.part_lse[base + tid] =
-            st[tid][1] > 0.0 ? (float)((st[tid][0] + log(st[tid][1])) * 1.4426950408889634) : -INFINITY;
+      for (int e = 0; e < PER; ++e) a.part_o[at * D + lane16 + 16 * e] = l > 0.0 ? (float)(o[e] / l) : 0.f;
+      if (lane16 == 0) a.part_lse[at] = l > 0.0 ? (float)((m + log(l)) * 1.4426950408889634) : -INFINITY;
     }
     if (end) break;
     advance<R, TK>(a, cu);
@@ -879,23 +876,28 @@ SharedPlan plan_shared(int B, int k, int Hq, int Hkv, int D, int G, int prefix_c
   int per_cu;
   if (dtype == 0) {
     p.rows_wg = kRowsF32;
-    per_cu = 4;
+    per_cu = 2;
   } else {
     // rows of an average group; a wave of two 16-row blocks halves the LDS reads
     // per product, eight such waves halve the HBM reads per row again
     const long long avg = (rows + G - 1) / G;
-    p.rows_wg = avg <= 128 ? 128 : 256;
+    p.rows_wg = 128;
+    auto places = [&](int rows_wg) {
+      return Hkv * (G * ((avg + rows_wg - 1) / rows_wg) * ((prefix_cap + kTile - 1) / kTile) +
+                    B * (long long)((kg + rows_wg - 1) / rows_wg) * ((cap + kTile - 1) / kTile + start_places(rows_wg)));
+    };
+    if (places(256) * 8 <= places(128) * 5) p.rows_wg = 256;
     per_cu = 1;
   }
   p.rows_own = std::min((kg + 15) / 16 * 16, p.rows_wg);
   const int own_tiles = (kg + p.rows_wg - 1) / p.rows_wg;
   const long long prefix_pairs = Hkv * (rows / p.rows_wg + G);
   const long long own_pairs = (long long)B * Hkv * own_tiles;
-  const int tk = p.rows_wg >= 128 ? kTileWide : kTileNarrow;
+  const int tk = p.rows_wg >= 128 ? kTile : kTileF32;
   const long long prefix_tiles = prefix_pairs * ((prefix_cap + tk - 1) / tk);
   const long long own_tiles_cap = own_pairs * ((cap + tk - 1) / tk);
   p.ok = prefix_tiles + own_tiles_cap + start_places(p.rows_wg) * (prefix_pairs + own_pairs) < (1LL << 30);
-  p.wgs = (int)std::max(1LL, std::min((long long)cus * per_cu, (prefix_tiles + own_tiles_cap) / 4));
+  p.wgs = (int)std::max(1LL, std::min((long long)cus * per_cu, prefix_tiles + own_tiles_cap));
   p.own_base = (prefix_pairs + p.wgs) * p.rows_wg;
   p.part_rows = (size_t)p.own_base + (size_t)(own_pairs + p.wgs) * p.rows_own;
   p.workspace_bytes = p.part_rows * ((size_t)D + 1) * sizeof(float);
@@ -910,14 +912,14 @@ hipError_t launch_shared(const SharedArgs& a, const SharedPlan& p, int dtype, hi
     else
       hipLaunchKernelGGL(shared_stream_f32<64>, dim3(p.wgs), dim3(256), 0, st, a, p.wgs);
     e = hipGetLastError();
-    return e != hipSuccess ? e : launch_merge<kRowsF32, kTileNarrow>(a, p, st);
+    return e != hipSuccess ? e : launch_merge<kRowsF32, kTileF32>(a, p, st);
   }
   if (p.rows_wg == 128) {
     e = a.D == 128 ? launch_wide<128, 1>(a, p, st) : launch_wide<64, 1>(a, p, st);
-    return e != hipSuccess ? e : launch_merge<128, kTileWide>(a, p, st);
+    return e != hipSuccess ? e : launch_merge<128, kTile>(a, p, st);
   }
   e = a.D == 128 ? launch_wide<128, 2>(a, p, st) : launch_wide<64, 2>(a, p, st);
-  return e != hipSuccess ? e : launch_merge<256, kTileWide>(a, p, st);
+  return e != hipSuccess ? e : launch_merge<256, kTile>(a, p, st);
 }
 
 }  // namespace sd
