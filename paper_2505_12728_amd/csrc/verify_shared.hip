@@ -45,12 +45,27 @@ constexpr int kTileF32 = 32, kTile = 64;   // keys per tile (fp32, bf16)
 // the one before) takes about as long as two tiles.
 constexpr int kRowsF32 = 16;
 constexpr int start_places(int rows_wg) { return rows_wg == kRowsF32 ? 0 : 2; }
-constexpr int kMergeWaves = 4096;   // rows of a sequence share a wave beyond that many
+constexpr int kMergeWaves = 8192;   // merge waves take several rows each beyond that many
+constexpr int kSplitRows = 1024;    // and four share a row up to that many
 constexpr float kHeadroom = 24.f;   // log2 of the largest weight before the maximum is raised
 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) const void gbl_cvoid;
 typedef const __attribute__((address_space(4))) int32_t cint32;   // scalar loads
+
+// Inclusive scan over the wave's 64 lanes by DPP moves (four shifts inside the
+// rows of 16 lanes, then the rows' last lanes to the rows behind), a tenth of
+// the latency of shuffles through LDS.  op(0, x) = x.
+template <typename Op>
+__device__ __forceinline__ int wave_scan(int v, Op op) {
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));   // row_shr:1
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));   // row_shr:2
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));   // row_shr:4
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));   // row_shr:8
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));   // row_bcast:15
+  return op(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));   // row_bcast:31
+}
+__device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
 
 // One unit of the list: a group's prefix (u < G) or a sequence's own cache
 // (sequence u - G).  first: its first sequence; end: the sequence behind its last.
@@ -107,14 +122,7 @@ __device__ __forceinline__ Span scan_units(const SharedArgs& a, int u0, Carry& c
   } else if (u < a.G + a.B) {
     s.un.L = min(max(a.kv_len[u - a.G], 0), a.cap);
   }
-  if (u0 < a.G) {
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int x = __shfl_up(bound, off, 64);   // (on every lane)
-      if (lane >= off) bound = max(bound, x);
-    }
-    bound = max(bound, c.bound);
-  }
+  if (u0 < a.G) bound = max(wave_scan(bound, [](int x, int y) { return max(x, y); }), c.bound);
   const int R = a.k * (a.Hq / a.Hkv);
   if (u < a.G) {
     s.un.first = bound;
@@ -125,73 +133,73 @@ __device__ __forceinline__ Span scan_units(const SharedArgs& a, int u0, Carry& c
     s.un.end = s.un.first + 1;
     s.un.rows = R;
   }
-  c.bound = max(c.bound, __shfl(bound, 63, 64));
+  c.bound = max(c.bound, last_lane(bound));
   s.pairs = a.Hkv * row_tiles(s.un.rows, ROWS);
   s.places = s.un.L > 0 ? s.pairs * (tiles_of<TK>(s.un.L) + start_places(ROWS)) : 0;
-  int ti = s.places, pi = s.pairs;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const int x = __shfl_up(ti, off, 64), y = __shfl_up(pi, off, 64);
-    if (lane >= off) {
-      ti += x;
-      pi += y;
-    }
-  }
+  auto add = [](int x, int y) { return x + y; };
+  const int ti = wave_scan(s.places, add), pi = wave_scan(s.pairs, add);
   s.n_before = c.places + ti - s.places;
   s.p_before = c.pairs + pi - s.pairs;
-  c.places += __shfl(ti, 63, 64);
-  c.pairs += __shfl(pi, 63, 64);
+  c.places += last_lane(ti);
+  c.pairs += last_lane(pi);
   return s;
 }
 
-// length T of the list
+// cursor of the first tile at place n or behind it, from the span that holds
+// place n.  The pair counts its kind only: own pairs start at 0 again.
 template <int ROWS, int TK>
-__device__ __forceinline__ int list_length(const SharedArgs& a) {
-  Carry c;
-  for (int u0 = 0; u0 < a.G + a.B; u0 += 64) scan_units<ROWS, TK>(a, u0, c);
-  return c.places;
+__device__ __forceinline__ Cursor tile_in(const SharedArgs& a, const Span& s, int u0, int n) {
+  constexpr int kStart = start_places(ROWS);
+  const int f = __builtin_ctzll(__ballot(s.n_before + s.places > n));
+  auto of = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
+  Cursor cu;
+  cu.u = u0 + f;
+  cu.L = of(s.un.L);
+  cu.rows = of(s.un.rows);
+  cu.first = of(s.un.first);
+  cu.end = of(s.un.end);
+  cu.nt = tiles_of<TK>(cu.L);
+  cu.RT = row_tiles(cu.rows, ROWS);
+  const int rem = n - of(s.n_before);
+  const int x = rem / (cu.nt + kStart);
+  cu.t = max(rem - x * (cu.nt + kStart) - kStart, 0);
+  cu.n = of(s.n_before) + x * (cu.nt + kStart) + kStart + cu.t;
+  cu.hk = x / cu.RT;
+  cu.rt = x - cu.hk * cu.RT;
+  cu.pair = cu.u < a.G ? of(s.p_before) + x : (cu.u - a.G) * a.Hkv * cu.RT + x;
+  return cu;
 }
 
-// cursor of the first tile at place n (0 <= n < T) or behind it.  The pair counts
-// its kind only: own pairs start at 0 again (R rows each).
+// The range of work-group w of G: its first tile and the place behind its last;
+// false: no tile.  In scalar registers (the compiler cannot see that the scan
+// ends alike on every lane), so that its bookkeeping stays off the vector unit.
 template <int ROWS, int TK>
-__device__ __forceinline__ Cursor find_tile(const SharedArgs& a, int n) {
+__device__ __forceinline__ bool first_tile(const SharedArgs& a, int w, int G, Cursor* first, int* behind) {
+  const int units = a.G + a.B;
   Carry c;
-  for (int u0 = 0; u0 < a.G + a.B; u0 += 64) {
-    const Span s = scan_units<ROWS, TK>(a, u0, c);
-    if (n >= c.places) continue;
-    const int f = __builtin_ctzll(__ballot(s.n_before + s.places > n));
-    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
-    Cursor cu;
-    cu.u = u0 + f;
-    cu.L = of(s.un.L);
-    cu.rows = of(s.un.rows);
-    cu.first = of(s.un.first);
-    cu.end = of(s.un.end);
-    cu.nt = tiles_of<TK>(cu.L);
-    cu.RT = row_tiles(cu.rows, ROWS);
-    constexpr int kStart = start_places(ROWS);
-    const int rem = n - of(s.n_before);
-    const int x = rem / (cu.nt + kStart);
-    cu.t = max(rem - x * (cu.nt + kStart) - kStart, 0);
-    cu.n = of(s.n_before) + x * (cu.nt + kStart) + kStart + cu.t;
-    cu.hk = x / cu.RT;
-    cu.rt = x - cu.hk * cu.RT;
-    cu.pair = cu.u < a.G ? of(s.p_before) + x : (cu.u - a.G) * a.Hkv * cu.RT + x;
-    return cu;
+  const Span s0 = scan_units<ROWS, TK>(a, 0, c);
+  for (int u0 = 64; u0 < units; u0 += 64) scan_units<ROWS, TK>(a, u0, c);
+  const int T = __builtin_amdgcn_readfirstlane(c.places);
+  const int n0 = (int)((long long)T * w / G), n1 = (int)((long long)T * (w + 1) / G);
+  if (n0 >= n1) return false;
+  Cursor cu{};
+  if (units <= 64) {
+    cu = tile_in<ROWS, TK>(a, s0, 0, n0);
+  } else {
+    Carry d;
+    for (int u0 = 0; u0 < units; u0 += 64) {
+      const Span s = scan_units<ROWS, TK>(a, u0, d);
+      if (n0 >= d.places) continue;
+      cu = tile_in<ROWS, TK>(a, s, u0, n0);
+      break;
+    }
   }
-  return Cursor{};   // n >= T: not reached
-}
-
-// the same in scalar registers (the compiler cannot see that the search ends
-// alike on every lane), so that its bookkeeping stays off the vector unit
-template <int ROWS, int TK>
-__device__ __forceinline__ Cursor locate(const SharedArgs& a, int n) {
-  Cursor cu = find_tile<ROWS, TK>(a, n);
   int* f[] = {&cu.n, &cu.u, &cu.hk, &cu.rt, &cu.t, &cu.nt, &cu.RT, &cu.L, &cu.rows, &cu.first, &cu.end, &cu.pair};
 #pragma unroll
   for (int* x : f) *x = __builtin_amdgcn_readfirstlane(*x);
-  return cu;
+  *first = cu;
+  *behind = n1;
+  return cu.n < n1;
 }
 
 // place of the tile behind cu
@@ -247,23 +255,13 @@ __device__ __forceinline__ int out_row(const SharedArgs& a, int first, int hk, i
   return (first * a.k + q) * a.Hq + hk * g + (r - q * g);
 }
 
-// ------------------------------------------------- bf16 stream, many rows
-// Eight waves of RB 16-row blocks on 64-key tiles, matrix-core bound.  A step
-// computes the scores of tile x + 1 under the exponentials of tile x, then P V
-// of tile x under the row maxima of tile x + 1, which are raised (rarely) after
-// it.  It runs in groups of four LDS fragments each: a group's reads are issued
-// one group ahead and waited for by count, and its matrix-core and vector
-// operations alternate.  K and V have rings of four slots; the tile that a step
-// copies lands two steps later.
-template <int ID, int MFMAS, int VALUS>
-__device__ __forceinline__ void alternate() {
-  if constexpr (MFMAS > 0) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, ID);
-    __builtin_amdgcn_sched_group_barrier(0x002, VALUS, ID);
-    alternate<ID, MFMAS - 1, VALUS>();
-  }
-}
-
+// ------------------------------------------------------------ bf16 stream
+// Eight waves of RB 16-row blocks on 64-key tiles.  A step computes the scores
+// of tile x + 1 under the exponentials of tile x, then P V of tile x under the
+// lane maxima of tile x + 1; the running maxima are raised (rarely) after it.  It
+// runs in groups of four LDS fragments: a group's reads are issued one group
+// ahead and waited for by count.  K and V have rings of four slots: a tile's copy
+// has two steps to land.
 template <int V>
 struct Const {
   static constexpr int value = V;
@@ -277,7 +275,7 @@ __device__ __forceinline__ void unrolled(F&& f) {
 }
 
 template <int D, int RB, bool HILO>
-__global__ __launch_bounds__(512, 2) void shared_wide_bf16(SharedArgs a, int G) {
+__global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G) {
   constexpr int NW = 8, TK = kTile, NBUF = 4;
   constexpr int DC = D / 32;                   // 32-channel slices (S^T = K Q^T)
   constexpr int DB = D / 16;                   // 16-channel blocks (O^T)
@@ -285,95 +283,124 @@ __global__ __launch_bounds__(512, 2) void shared_wide_bf16(SharedArgs a, int G) 
   constexpr int ROW = D * 2;
   constexpr int HALF = TK * ROW;               // a tile's K (or V)
   constexpr int KEYS = 64 / PK;                // keys of one 64-lane copy
-  constexpr int COPIES = TK / KEYS / NW;       // per wave and half
+  constexpr int COPIES = TK / KEYS / NW;       // per wave and half: 8 keys a wave
+  constexpr int TILE_COPIES = 2 * COPIES;
   constexpr int ROWS = NW * RB * 16;
   constexpr int KPG = 4 / DC;                  // 16-key blocks of a score group
   constexpr int NQK = 4 / KPG, NPVH = DB / 4, NG = NQK + 2 * NPVH;
   static_assert(NBUF * HALF <= 65536, "ring slots within the LDS instructions' offsets");
+  static_assert(COPIES * KEYS == 8, "a wave copies 8 keys, which lie in one page");
   __shared__ __align__(16) unsigned char ring[2][NBUF * HALF];   // K, V
 
   const int lane = threadIdx.x & 63, G4 = lane >> 4, c = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wg = blockIdx.x;
-  const int T = __builtin_amdgcn_readfirstlane(list_length<ROWS, TK>(a));
-  const int n0 = (int)((long long)T * wg / G), n1 = (int)((long long)T * (wg + 1) / G);
-  if (n0 >= n1) return;
-  Cursor cc = locate<ROWS, TK>(a, n0);
-  if (cc.n >= n1) return;
+  Cursor cc;
+  int n1;
+  if (!first_tile<ROWS, TK>(a, wg, G, &cc, &n1)) return;
 
-  // copy i of this wave takes keys (w COPIES + i) KEYS .. of K and of V; a lane's
-  // 16-byte piece goes to LDS slot piece ^ lds_swizzle(key).  A copy's keys lie in
-  // one page.  Keys past the unit's length re-read its last key (masked).
-  int ckey[COPIES];
-  uint32_t cpiece[COPIES];
-#pragma unroll
-  for (int i = 0; i < COPIES; ++i) {
-    ckey[i] = (w * COPIES + i) * KEYS + lane / PK;
-    cpiece[i] = ((lane % PK) ^ lds_swizzle<PK>(ckey[i])) * 16;
-  }
-  // the tile that is copied next: its first keys' byte offsets in the caches
-  // (found one step ahead, as page ids are loads) and its last key
-  size_t cbase[COPIES];
-  int clast = 0, cstep = 0;
-  const unsigned char *ck = nullptr, *cv = nullptr;
-  auto place = [&](const Cursor& cu) {
-    const bool own = cu.u >= a.G;
-    const int row = own ? cu.first : cu.u;
-    ck = static_cast<const unsigned char*>(own ? a.k_cache : a.k_prefix);
-    cv = static_cast<const unsigned char*>(own ? a.v_cache : a.v_prefix);
+  // Copies.  This wave takes keys 8 w .. 8 w + 7 of a tile's K and V; a lane's
+  // 16-byte piece goes to LDS slot piece ^ lds_swizzle(key).  Keys past the
+  // unit's length re-read its last key (masked).  cur: the tile copied next.
+  // (The swizzle of key + 4 differs in bit 3 where a wave takes two copies.)
+  const int ckey = lane / PK;
+  const uint32_t cpiece = ((lane % PK) ^ lds_swizzle<PK>(w * 8 + ckey)) * 16;
+  static_assert(COPIES == 1 || lds_swizzle<PK>(4) == 8, "second copy's piece");
+  Cursor ic = cc;
+  const unsigned char *ck = nullptr, *cv = nullptr;   // of the pair: its keys and values
+  cint32* cpages = nullptr;                    // its row of the page table
+  int cpool = 0, cstep = 0, clim = 0;          // pages of the pool, bytes between keys, last key of the 8
+  size_t cbase = 0;                            // offset of the wave's keys
+  auto enter_pair = [&]() {
+    const bool own = ic.u >= a.G;
+    const int row = own ? ic.first : ic.u;
     const int32_t* table = own ? a.page_table : a.prefix_table;
-    const int t0 = cu.t * TK;
-    clast = cu.L - 1 - t0;
+    size_t at;
     if (table != nullptr) {
-      const int pages = own ? a.num_pages : a.prefix_num_pages;
-      cint32* pt = (cint32*)(table + (size_t)row * (own ? a.max_pages : a.prefix_pages));
-      const int lastp = (cu.L - 1) >> 4;
+      cpages = (cint32*)(table + (size_t)row * (own ? a.max_pages : a.prefix_pages));
+      cpool = own ? a.num_pages : a.prefix_num_pages;
       cstep = ROW;
-#pragma unroll
-      for (int i = 0; i < COPIES; ++i) {
-        const int key0 = (w * COPIES + i) * KEYS;
-        const int pi = min((t0 + key0) >> 4, lastp);
-        const int page = min(max((int)pt[pi], 0), pages - 1);
-        // offset of the tile's key 0 as if every key lay in this page
-        cbase[i] = (((size_t)page * a.Hkv + cu.hk) * 16) * ROW - (size_t)(pi * 16 - t0) * ROW;
-      }
+      at = (size_t)ic.hk * (16 * ROW);
     } else {
+      cpages = nullptr;
       cstep = a.Hkv * ROW;
-#pragma unroll
-      for (int i = 0; i < COPIES; ++i)
-        cbase[i] = (((size_t)row * (own ? a.Lmax : a.prefix_cap) + t0) * a.Hkv + cu.hk) * ROW;
+      at = ((size_t)row * (own ? a.Lmax : a.prefix_cap) * a.Hkv + ic.hk) * ROW;
+    }
+    ck = static_cast<const unsigned char*>(own ? a.k_cache : a.k_prefix) + at;
+    cv = static_cast<const unsigned char*>(own ? a.v_cache : a.v_prefix) + at;
+  };
+  auto enter_tile = [&]() {
+    const int key0 = min(ic.t * TK + w * 8, (ic.L - 1) & ~7);
+    clim = ic.L - 1 - key0;
+    if (cpages != nullptr) {
+      const int page = min(max((int)cpages[key0 >> 4], 0), cpool - 1);
+      cbase = (size_t)page * (size_t)(a.Hkv * 16 * ROW) + (key0 & 15) * ROW;
+    } else {
+      cbase = (size_t)key0 * (size_t)cstep;
     }
   };
-  auto issue = [&](int slot) {
+  // the copy of one tile, and the step to the next; past the range the last one
+  // is copied again
+  auto copy_next = [&](int slot) {
 #pragma unroll
     for (int i = 0; i < COPIES; ++i) {
-      const uint32_t off = (uint32_t)min(ckey[i], clast) * (uint32_t)cstep + cpiece[i];
+      const size_t off = cbase + ((uint32_t)min(ckey + i * KEYS, clim) * (uint32_t)cstep + (cpiece ^ (i * 128)));
       const int at = slot * HALF + (w * COPIES + i) * 1024;
-      __builtin_amdgcn_global_load_lds((gbl_cvoid*)(ck + cbase[i] + off), (lds_void*)(ring[0] + at), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((gbl_cvoid*)(cv + cbase[i] + off), (lds_void*)(ring[1] + at), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((gbl_cvoid*)(ck + off), (lds_void*)(ring[0] + at), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((gbl_cvoid*)(cv + off), (lds_void*)(ring[1] + at), 16, 0, 0);
+    }
+    if (place_behind<ROWS>(ic) < n1) {
+      advance<ROWS, TK>(a, ic);
+      if (ic.t == 0) enter_pair();
+      enter_tile();
     }
   };
 
   // fragment addresses for the first 16 keys of slot 0 (the swizzle depends on
-  // key % 16 only, so further blocks and slots are offsets)
-  uint32_t kaddr[DC], vaddr[DB];
+  // key % 16 only, so further blocks and slots are offsets).  K: 16 keys x one
+  // piece; V, transposed: lane j of group G4 addresses key 4 G4 + j / 4 at
+  // channels db * 16 + 4 (j % 4) and receives 4 keys at channel db * 16 + c.
+  // Blocks db and db + 4 differ in bit 7 of the address (128 bytes of a row).
+  uint32_t kaddr[DC], vaddr[4];
 #pragma unroll
   for (int dc = 0; dc < DC; ++dc)
     kaddr[dc] = lds_addr(ring[0]) + c * ROW + (((dc * 4 + G4) ^ lds_swizzle<PK>(c)) * 16);
 #pragma unroll
-  for (int db = 0; db < DB; ++db) {
+  for (int db = 0; db < 4; ++db) {
     const int key = 4 * G4 + (c >> 2), ch = db * 16 + 4 * (c & 3);
     vaddr[db] = lds_addr(ring[1]) + key * ROW + (((ch >> 3) ^ lds_swizzle<PK>(key)) * 16) + (ch & 7) * 2;
   }
 
-  // segment state (rows, maxima and sums as in the narrow kernel)
+  // Segment state: queries (B operand of S^T = K Q^T), last visible keys, running
+  // (max, sum, O^T) and the raw scores of the tile whose turn it is.  The scale
+  // enters the exponents as exp2(S sl2 - m); a negative one is folded into the
+  // queries.
   bf16x8 qf[RB][DC];
   int lim[RB];
   float m[RB], l[RB];
-  floatx4 o[RB][DB], sc[4][RB];                // sc: raw scores of the tile whose turn it is
+  floatx4 o[RB][DB], sc[4][RB];
   const bool neg = a.scale_log2 < 0.f;
   const float sl2 = fabsf(a.scale_log2);
   const int g = a.Hq / a.Hkv, kg = a.k * g;
+  // queries of the pair under cursor cu; true if this wave has rows of it
+  auto load_rows = [&](const Cursor& cu) {
+    const int r0 = cu.rt * ROWS + w * RB * 16;
+    if (r0 >= cu.rows) return false;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int r = r0 + rb * 16 + c;
+      const bool here = r < cu.rows;
+      const u32x4* src = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q) +
+                                                        (size_t)out_row(a, cu.first, cu.hk, here ? r : r0) * D);
+#pragma unroll
+      for (int dc = 0; dc < DC; ++dc) {
+        Pack8 pk;
+        pk.u = src[dc * 4 + G4];
+        qf[rb][dc] = pk.b;
+      }
+    }
+    return true;
+  };
 
   u32x4 xr[2][4];
   u32x2 vr[2][4][2];
@@ -396,50 +423,47 @@ __global__ __launch_bounds__(512, 2) void shared_wide_bf16(SharedArgs a, int G) 
           tie(vr[gr & 1][d][0]);
           tie(vr[gr & 1][d][1]);
         } else {
-          vr[gr & 1][d][0] = lds_read_tr16_b64_off<PH * HALF + hf * 32 * ROW>(vaddr[4 * pb + d] + dh);
-          vr[gr & 1][d][1] = lds_read_tr16_b64_off<PH * HALF + hf * 32 * ROW + 16 * ROW>(vaddr[4 * pb + d] + dh);
+          const uint32_t at = (vaddr[d] ^ (pb * 128)) + dh;
+          vr[gr & 1][d][0] = lds_read_tr16_b64_off<PH * HALF + hf * 32 * ROW>(at);
+          vr[gr & 1][d][1] = lds_read_tr16_b64_off<PH * HALF + hf * 32 * ROW + 16 * ROW>(at);
         }
       });
     }
   };
-
-  // maxima of the raw scores in s, raised where a weight would pass 2^24 (or at once)
-  auto raise = [&](const floatx4 (&s)[4][RB], bool at_once) {
-    float lm[RB];
-    bool over = at_once;
+  // scores of score group gr from its fragments
+  auto scores = [&](auto gtag, floatx4 (&s)[4][RB]) {
+    constexpr int gr = decltype(gtag)::value;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      lm[rb] = s[0][rb][0];
+    for (int kk = 0; kk < KPG; ++kk) {
+      const int kb = gr * KPG + kk;
 #pragma unroll
-      for (int kb = 0; kb < 4; ++kb)
+      for (int dc = 0; dc < DC; ++dc) {
+        Pack8 pk;
+        pk.u = xr[gr & 1][kk * DC + dc];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) lm[rb] = fmaxf(lm[rb], s[kb][rb][i]);
-      over = over || fmaf(lm[rb], sl2, -m[rb]) > kHeadroom;
-    }
-    if (__ballot(over) == 0ull) return;
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const float top = wave_max_across_groups(lm[rb]) * sl2;
-      const float mnew = at_once ? top : fmaxf(m[rb], top);
-      const float f = at_once ? 0.f : fast_exp2(m[rb] - mnew);   // O and l are 0 at the start
-      l[rb] *= f;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) o[rb][db] *= f;
-      m[rb] = mnew;
+        for (int rb = 0; rb < RB; ++rb)
+          s[kb][rb] = mfma_bf16(pk.b, qf[rb][dc], dc == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : s[kb][rb]);
+      }
     }
   };
+  auto lane_max = [&](const floatx4& s, float top) {
+    return fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), top);
+  };
 
-  // One step, tile x of the segment: NEXT: there is a tile x + 1 in it; MASK: a
-  // row's last visible key may lie in tile x (first key t0).  PH: ring phase of
-  // x where known (the slots then sit in the instructions' offsets), else -1.
-  auto step = [&](int n, int t0, auto ph_tag, auto next_tag, auto mask_tag) {
+  // One step, tile t0 / TK of the segment at ring step x.  NEXT: there is a tile
+  // behind it in the segment.  MASK: a row's last visible key may lie in the tile.
+  // PH: x % NBUF where known (the slots then sit in the instructions' offsets),
+  // else -1.
+  auto step = [&](int x, int t0, auto ph_tag, auto next_tag, auto mask_tag) {
     constexpr int PH = decltype(ph_tag)::value;
     constexpr bool NEXT = decltype(next_tag)::value, MASK = decltype(mask_tag)::value;
-    constexpr int PN0 = PH >= 0 ? (PH + 1) % NBUF : 0, PH0 = PH >= 0 ? PH : 0;
-    const uint32_t dn = PH >= 0 ? 0u : (uint32_t)((n + 1) % NBUF) * HALF, dh = PH >= 0 ? 0u : (uint32_t)(n % NBUF) * HALF;
+    constexpr int PN = PH >= 0 ? (PH + 1) % NBUF : 0, P0 = PH >= 0 ? PH : 0;
+    const uint32_t dh = PH >= 0 ? 0u : (uint32_t)(x % NBUF) * HALF;
+    const uint32_t dn = PH >= 0 ? 0u : (uint32_t)((x + 1) % NBUF) * HALF;
     constexpr int G0 = NEXT ? 0 : NQK;         // the last tile has no scores to form
     bf16x8 ph[2][RB], pl[2][RB];
     floatx4 sn[4][RB];
+    float lm[RB];
     auto weights = [&](int kb) {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
@@ -457,33 +481,26 @@ __global__ __launch_bounds__(512, 2) void shared_wide_bf16(SharedArgs a, int G) 
         l[rb] += (p[0] + p[1]) + (p[2] + p[3]);
       }
     };
-    reads(Const<G0>{}, Const<PN0>{}, Const<PH0>{}, dn, dh, Const<0>{});
+    // tile x + 1 has landed (its wait leaves tile x + 2's copy under way), tile
+    // x - 1's slot is free
+    wait_vm_then_barrier<TILE_COPIES>();
+    copy_next(PH >= 0 ? (PH + 3) % NBUF : (x + 3) % NBUF);
+    reads(Const<G0>{}, Const<PN>{}, Const<P0>{}, dn, dh, Const<0>{});
     if constexpr (!NEXT) {
 #pragma unroll
       for (int kb = 0; kb < 4; ++kb) weights(kb);
     }
     unrolled<G0, NG>([&](auto gtag) {
       constexpr int gr = decltype(gtag)::value;
-      reads(Const<gr + 1>{}, Const<PN0>{}, Const<PH0>{}, dn, dh, Const<0>{});
+      reads(Const<gr + 1>{}, Const<PN>{}, Const<P0>{}, dn, dh, Const<0>{});
       lds_wait_n<(gr + 1 < NQK ? 4 : gr + 1 < NG ? 8 : 0)>();
-      reads(gtag, Const<PN0>{}, Const<PH0>{}, dn, dh, Const<1>{});
+      reads(gtag, Const<PN>{}, Const<P0>{}, dn, dh, Const<1>{});
       if constexpr (gr < NQK) {
+        scores(gtag, sn);
 #pragma unroll
-        for (int kk = 0; kk < KPG; ++kk) {
-          const int kb = gr * KPG + kk;
-#pragma unroll
-          for (int dc = 0; dc < DC; ++dc) {
-            Pack8 pk;
-            pk.u = xr[gr & 1][kk * DC + dc];
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-              sn[kb][rb] = mfma_bf16(pk.b, qf[rb][dc], dc == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : sn[kb][rb]);
-          }
-          weights(kb);
-        }
-        alternate<gr + 1, 4 * RB, HILO ? 6 : 3>();
+        for (int kk = 0; kk < KPG; ++kk) weights(gr * KPG + kk);
       } else {
-        constexpr int q = gr - NQK, hf = q / NPVH, pb = q % NPVH;
+        constexpr int q = gr - NQK, hf = q / NPVH, pb = q % NPVH, per = 4 / (2 * NPVH);
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
           Pack8 vv;
@@ -494,11 +511,33 @@ __global__ __launch_bounds__(512, 2) void shared_wide_bf16(SharedArgs a, int G) 
             if constexpr (HILO) o[rb][4 * pb + d] = mfma_bf16(vv.b, pl[hf][rb], o[rb][4 * pb + d]);
           }
         }
+        if constexpr (NEXT) {
+#pragma unroll
+          for (int kb = q * per; kb < (q + 1) * per; ++kb)
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) lm[rb] = lane_max(sn[kb][rb], kb == 0 ? sn[0][rb][0] : lm[rb]);
+        }
       }
       __builtin_amdgcn_sched_barrier(0);
     });
     if constexpr (NEXT) {
-      raise(sn, false);
+      // A lane's largest exponent, taken before the mask, bounds the masked ones;
+      // m, raised only where it passes 2^24, may so exceed the true maximum,
+      // which cancels in o = O / l and lse = m + log2 l
+      bool over = false;
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) over = over || fmaf(lm[rb], sl2, -m[rb]) > kHeadroom;
+      if (__ballot(over) != 0ull) {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+          const float top = fmaxf(m[rb], wave_max_across_groups(lm[rb]) * sl2);
+          const float f = fast_exp2(m[rb] - top);
+          l[rb] *= f;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) o[rb][db] *= f;
+          m[rb] = top;
+        }
+      }
 #pragma unroll
       for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
@@ -506,121 +545,94 @@ __global__ __launch_bounds__(512, 2) void shared_wide_bf16(SharedArgs a, int G) 
     }
   };
 
-  // Ring: entering the step of tile n the copies of tiles n + 1 and n + 2 are
-  // under way; the wait leaves tile n + 2's, the barrier frees tile n - 1's slot
-  // for tile n + 3.  Past the range the last tile is copied again.
-  Cursor ic = cc;
-  place(ic);
-  auto copy_next = [&](int slot) {
-    issue(slot);
-    if (place_behind<ROWS>(ic) < n1) {
-      advance<ROWS, TK>(a, ic);
-      place(ic);
-    }
-  };
+  enter_pair();
+  enter_tile();
+  bool busy = load_rows(cc);
 #pragma unroll 1
   for (int i = 0; i < NBUF - 1; ++i) copy_next(i);
-  wait_vm_then_barrier<2 * 2 * COPIES>();      // tile n0 is there
-  auto begin = [&](int x) {                    // step x of the ring
-    wait_vm_then_barrier<2 * COPIES>();
-    copy_next((x + NBUF - 1) % NBUF);
-  };
-
   int x = 0;                                   // ring step
   while (true) {
-    const bool own = cc.u >= a.G;
-    const int rt = cc.rt, rows = cc.rows, pair = cc.pair;
     const int steps = min(cc.nt - cc.t, n1 - cc.n);
     const int t_first = cc.t * TK;
-    // tiles before the first with masked keys, and before the last
-    const int unmasked = own ? cc.L - a.k : cc.L - 1;
-    const int plain = max(0, min(steps - 1, (unmasked + 1) / TK - cc.t));
-    const int r0 = rt * ROWS + w * RB * 16;
-    if (r0 < rows) {
+    const Cursor seg = cc;
+    cc.t += steps - 1;
+    cc.n += steps - 1;
+    const bool more = place_behind<ROWS>(cc) < n1;
+    if (more) advance<ROWS, TK>(a, cc);        // the next segment
+    if (x == 0) wait_vm_then_barrier<2 * TILE_COPIES>();   // the first tile has landed
+    if (busy) {
+      if (neg) {
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        const int r = r0 + rb * 16 + c;
-        Pack8 pk;
-        pk.u = u32x4{0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int dc = 0; dc < DC; ++dc) qf[rb][dc] = pk.b;
-        lim[rb] = -1;
-        if (r < rows) {
-          const u32x4* src = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q) +
-                                                            (size_t)out_row(a, cc.first, cc.hk, r) * D);
-#pragma unroll
-          for (int dc = 0; dc < DC; ++dc) {
-            pk.u = src[dc * 4 + G4];
-            if (neg) pk.u ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
-            qf[rb][dc] = pk.b;
-          }
-          lim[rb] = own ? cc.L - a.k + (r % kg) / g : cc.L - 1;
-        }
-        l[rb] = 0.f;
-        m[rb] = 0.f;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) o[rb][db] = floatx4{0.f, 0.f, 0.f, 0.f};
-      }
-      __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));   // vmcnt(0): the counted waits only see copies
-      // scores of the first tile
-      const uint32_t d0 = (uint32_t)(x % NBUF) * HALF;
-      unrolled<0, NQK>([&](auto gtag) {
-        constexpr int gr = decltype(gtag)::value;
-        reads(gtag, Const<0>{}, Const<0>{}, d0, 0u, Const<0>{});
-        lds_wait();
-        reads(gtag, Const<0>{}, Const<0>{}, d0, 0u, Const<1>{});
-#pragma unroll
-        for (int kk = 0; kk < KPG; ++kk)
+        for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
           for (int dc = 0; dc < DC; ++dc) {
             Pack8 pk;
-            pk.u = xr[gr & 1][kk * DC + dc];
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-              sc[gr * KPG + kk][rb] =
-                  mfma_bf16(pk.b, qf[rb][dc], dc == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : sc[gr * KPG + kk][rb]);
+            pk.b = qf[rb][dc];
+            pk.u ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
+            qf[rb][dc] = pk.b;
           }
-      });
-      raise(sc, true);
-      int i = 0;                               // step of the segment
-#define SD_STEP(PH, NEXT, MASK)                                                                 \
-  {                                                                                             \
-    begin(x);                                                                                   \
-    step(x, t_first + i * TK, Const<PH>{}, Const<NEXT>{}, Const<MASK>{});                       \
-    ++x;                                                                                        \
-    ++i;                                                                                        \
-  }
-      while (i < plain && x % NBUF != 0) SD_STEP(-1, 1, 0)
-      while (i + NBUF <= plain) {
-        SD_STEP(0, 1, 0)
-        SD_STEP(1, 1, 0)
-        SD_STEP(2, 1, 0)
-        SD_STEP(3, 1, 0)
       }
-      while (i < plain) SD_STEP(-1, 1, 0)
-      while (i < steps - 1) SD_STEP(-1, 1, 1)
-      SD_STEP(-1, 0, 1)
-#undef SD_STEP
-      // the segment's partial
+      // scores of the first tile, and their maxima
+      const uint32_t d0 = (uint32_t)(x % NBUF) * HALF;
+      unrolled<0, NQK>([&](auto gtag) {
+        reads(gtag, Const<0>{}, Const<0>{}, d0, 0u, Const<0>{});
+        lds_wait();
+        reads(gtag, Const<0>{}, Const<0>{}, d0, 0u, Const<1>{});
+        scores(gtag, sc);
+      });
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        const float lsum = wave_sum_across_groups(l[rb]);
-        const int lr = (w * RB + rb) * 16 + c;
-        if (rt * ROWS + lr >= rows) continue;
-        const size_t prow = part_row<ROWS>(a, own, pair, wg) + lr;
-        const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+        float top = sc[0][rb][0];
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
-          *reinterpret_cast<floatx4*>(a.part_o + prow * D + db * 16 + 4 * G4) = o[rb][db] * inv;
-        if (G4 == 0) a.part_lse[prow] = lsum > 0.f ? m[rb] + log2f(lsum) : -INFINITY;
+        for (int kb = 0; kb < 4; ++kb) top = lane_max(sc[kb][rb], top);
+        m[rb] = wave_max_across_groups(top) * sl2;
+        l[rb] = 0.f;
+        const int r = seg.rt * ROWS + (w * RB + rb) * 16 + c;
+        lim[rb] = seg.u >= a.G ? seg.L - a.k + r % kg / g : seg.L - 1;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[rb][db] = floatx4{0.f, 0.f, 0.f, 0.f};
       }
-    } else {
-      for (int i = 0; i < steps; ++i) begin(x++);   // no rows: its copies only
     }
-    cc.t += steps - 1;
-    cc.n += steps - 1;
-    if (place_behind<ROWS>(cc) >= n1) break;
-    advance<ROWS, TK>(a, cc);
+    if (!busy) {
+      for (int i = 0; i < steps; ++i, ++x) {   // no rows: its copies only
+        wait_vm_then_barrier<TILE_COPIES>();
+        copy_next((x + 3) % NBUF);
+      }
+      busy = more && load_rows(cc);
+      if (!more) break;
+      continue;
+    }
+    int i = 0;                                 // step of the segment
+    // (only the last two tiles of a segment can hold masked keys: k <= 16)
+    for (; i < steps - 2 && x % NBUF != 0; ++i, ++x) step(x, 0, Const<-1>{}, Const<1>{}, Const<0>{});
+    for (; i + NBUF <= steps - 2; i += NBUF, x += NBUF) {
+      step(x, 0, Const<0>{}, Const<1>{}, Const<0>{});
+      step(x, 0, Const<1>{}, Const<1>{}, Const<0>{});
+      step(x, 0, Const<2>{}, Const<1>{}, Const<0>{});
+      step(x, 0, Const<3>{}, Const<1>{}, Const<0>{});
+    }
+    for (; i < steps - 2; ++i, ++x) step(x, 0, Const<-1>{}, Const<1>{}, Const<0>{});
+    if (i < steps - 1) {
+      step(x, t_first + i * TK, Const<-1>{}, Const<1>{}, Const<1>{});
+      ++i;
+      ++x;
+    }
+    step(x, t_first + i * TK, Const<-1>{}, Const<0>{}, Const<1>{});
+    ++x;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const float lsum = wave_sum_across_groups(l[rb]);
+      const int lr = (w * RB + rb) * 16 + c;
+      if (seg.rt * ROWS + lr >= seg.rows) continue;
+      const size_t prow = part_row<ROWS>(a, seg.u >= a.G, seg.pair, wg) + lr;
+      const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        *reinterpret_cast<floatx4*>(a.part_o + prow * D + db * 16 + 4 * G4) = o[rb][db] * inv;
+      if (G4 == 0) a.part_lse[prow] = lsum > 0.f ? m[rb] + log2f(lsum) : -INFINITY;
+    }
+    if (!more) break;
+    busy = load_rows(cc);
   }
   __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));   // no copy may still write this LDS
 }
@@ -640,11 +652,9 @@ __global__ __launch_bounds__(256) void shared_stream_f32(SharedArgs a, int G) {
   __shared__ double ps[R][TK + 1];             // weights
   const int tid = threadIdx.x, r = tid >> 4, lane16 = tid & 15;
   const int wg = blockIdx.x;
-  const int T = list_length<R, TK>(a);
-  const int n0 = (int)((long long)T * wg / G), n1 = (int)((long long)T * (wg + 1) / G);
-  if (n0 >= n1) return;
-  Cursor cu = locate<R, TK>(a, n0);
-  if (cu.n >= n1) return;
+  Cursor cu;
+  int n1;
+  if (!first_tile<R, TK>(a, wg, G, &cu, &n1)) return;
   const int kg = a.k * (a.Hq / a.Hkv);
   double o[PER], m = -INFINITY, l = 0.0;
   bool fresh = true;
@@ -734,21 +744,25 @@ __global__ __launch_bounds__(256) void shared_stream_f32(SharedArgs a, int G) {
 }
 
 // ------------------------------------------------------------------ merge
-// One wave per output row.  The tiles at places [U, U + nt) lie with work-groups
-// owner(U) .. owner(U + nt - 1), owner(n) = floor(((n + 1) G - 1) / T), each of
-// which wrote one partial (with fewer places than work-groups, each owner did).  Candidates of the prefix pair, then of the own pair,
-// are taken 32 at a time: lanes 0..31 load their lse while each half-wave loads
-// the outputs of 16 of them (4 channels per lane), and the chunk's weights
-// 2^(lse - max) rescale a running sum.  Every shuffle runs on all lanes.
-// A wave takes `per` rows of one sequence, so that the scan over the units is
-// made once for them.
-template <int ROWS, int TK>
+// The tiles at places [U, U + nt) of a pair lie with work-groups owner(U) ..
+// owner(U + nt - 1), owner(n) = floor(((n + 1) G - 1) / T), each of which wrote
+// one partial (with fewer places than work-groups, each owner did).  A row's
+// candidates are the partials of its prefix pair, then of its own pair.  A wave
+// holds the row's channels (D / 64 per lane) and takes 8 candidates at a time:
+// their lse are the same on every lane, so that their weights 2^(lse - max) need
+// no exchange between lanes.  Few rows have many candidates each and take the
+// four waves of a work-group (SPLIT), joined in LDS; otherwise a wave takes
+// `per` rows of one sequence, so that the scan over the units is made once for
+// them.  Bound by latency while rows are few, by the partials' bytes beyond.
+template <int ROWS, int TK, int D, bool SPLIT>
 __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G, int per, int wgs_seq) {
+  constexpr int CH = D / 64, ROUND = 8;
+  __shared__ float part[4][2 + D];             // SPLIT: each wave's max, sum and channels
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int b = blockIdx.x / wgs_seq;
-  const int row0 = ((blockIdx.x - b * wgs_seq) * 4 + w) * per;   // of the k Hq rows of sequence b
-  if (row0 >= a.k * a.Hq) return;
-  const int D = a.D, g = a.Hq / a.Hkv;
+  const int row0 = ((blockIdx.x - b * wgs_seq) * (SPLIT ? 1 : 4) + (SPLIT ? 0 : w)) * per;   // of the k Hq rows of b
+  const int rows = a.k * a.Hq, row1 = min(row0 + per, rows);
+  const int g = a.Hq / a.Hkv;
 
   // places before the unit, key tiles, pairs before it, row tiles and first row
   // of the sequence, for the group's prefix (0) and the sequence's own keys (1)
@@ -772,98 +786,149 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G, int per
     }
   }
   const int T = c.places;
-  auto owner = [&](int n) { return (int)((((long long)n + 1) * G - 1) / T); };
   const bool sparse = T < G;   // then a work-group has one place or none: a candidate per tile
-  for (int row = row0; row < min(row0 + per, a.k * a.Hq); ++row) {
-  const int j = row / a.Hq, h = row - j * a.Hq, hk = h / g;
-  const size_t orow = (size_t)b * a.k * a.Hq + row;
-  int U[2], pair[2], lr[2], wf[2] = {0, 0}, nc[2] = {0, 0};
+  // ((n + 1) G - 1) / T: the float64 quotient is off by less than one
+  const double inv_t = 1.0 / (double)max(T, 1);
+  auto owner = [&](int n) {
+    const long long x = (long long)(n + 1) * G - 1;
+    const int q = (int)((double)x * inv_t);
+    const long long r = x - (long long)q * T;
+    return q + (r >= T) - (r < 0);
+  };
+  for (int row = row0; row < row1; ++row) {
+    const int j = row / a.Hq, h = row - j * a.Hq, hk = h / g;
+    int U[2], nc[2] = {0, 0}, wf[2] = {0, 0};
+    long long first[2] = {0, 0};               // partial row that work-group 0 would write for the pair
 #pragma unroll
-  for (int kind = 0; kind < 2; ++kind) {
-    const int r = base[kind] + j * g + (h - hk * g);
-    const int x = hk * RT[kind] + r / ROWS;
-    U[kind] = before[kind] + x * (nt[kind] + start_places(ROWS)) + start_places(ROWS);
-    pair[kind] = pairs[kind] + x;
-    lr[kind] = r % ROWS;
-    if (nt[kind] == 0) continue;
-    wf[kind] = owner(U[kind]);
-    nc[kind] = sparse ? nt[kind] : owner(U[kind] + nt[kind] - 1) - wf[kind] + 1;
-  }
-  auto writer = [&](int kind, int i) { return sparse ? owner(U[kind] + i) : wf[kind] + i; };
-  const int half = lane >> 5, d4 = lane & 31;
-  const bool active = d4 < D / 4;
-  floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-  float mx = -INFINITY, wsum = 0.f;
-  const int ncand = nc[0] + nc[1];
-  for (int c0 = 0; c0 < ncand; c0 += 32) {
-    const int n = min(32, ncand - c0);
-    // partial row of candidate c0 + i
-    auto prow = [&](int i) {
-      const int cand = c0 + i;
-      const bool own = cand >= nc[0];
-      return own ? part_row<ROWS>(a, true, pair[1], writer(1, cand - nc[0])) + lr[1]
-                 : part_row<ROWS>(a, false, pair[0], writer(0, cand)) + lr[0];
-    };
-    const float ls = lane < n ? a.part_lse[prow(lane)] : -INFINITY;
-    floatx4 po[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int j = 2 * i + half;
-      po[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-      if (j < n && active) po[i] = *reinterpret_cast<const floatx4*>(a.part_o + prow(j) * D + d4 * 4);
+    for (int kind = 0; kind < 2; ++kind) {
+      const int r = base[kind] + j * g + (h - hk * g);
+      const int x = hk * RT[kind] + r / ROWS;
+      U[kind] = before[kind] + x * (nt[kind] + start_places(ROWS)) + start_places(ROWS);
+      first[kind] = (long long)part_row<ROWS>(a, kind == 1, pairs[kind] + x, 0) + r % ROWS;
+      if (nt[kind] == 0) continue;
+      wf[kind] = owner(U[kind]);
+      nc[kind] = sparse ? nt[kind] : owner(U[kind] + nt[kind] - 1) - wf[kind] + 1;
     }
-    float cm = ls;
+    const int ncand = nc[0] + nc[1];
+    float mx = -INFINITY, wsum = 0.f, acc[CH];
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) cm = fmaxf(cm, __shfl_xor(cm, off, 64));
-    const float nm = fmaxf(mx, __shfl(cm, 0, 64));
-    if (nm == -INFINITY) continue;             // no key in any partial so far (uniform)
-    const float keep = mx == -INFINITY ? 0.f : exp2f(mx - nm);
-    const float wl = ls == -INFINITY ? 0.f : exp2f(ls - nm);
-    float ws = wl;
+    for (int e = 0; e < CH; ++e) acc[e] = 0.f;
+    for (int c0 = SPLIT ? w * ROUND : 0; c0 < ncand; c0 += SPLIT ? 4 * ROUND : ROUND) {
+      float ls[ROUND], po[ROUND][CH];
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) ws += __shfl_xor(ws, off, 64);
-    wsum = wsum * keep + __shfl(ws, 0, 64);
-    acc = acc * keep;
+      for (int i = 0; i < ROUND; ++i) {
+        const int cand = min(c0 + i, ncand - 1);
+        const int kind = cand >= nc[0], k = cand - (kind ? nc[0] : 0);
+        const int wv = sparse ? owner(U[kind] + k) : wf[kind] + k;
+        const size_t prow = (size_t)(first[kind] + (long long)wv * (kind ? a.rows_own : ROWS));
+        ls[i] = a.part_lse[prow];
+        const float* src = a.part_o + prow * D + lane * CH;
+        if constexpr (CH == 2) {
+          const float2 v = *reinterpret_cast<const float2*>(src);
+          po[i][0] = v.x;
+          po[i][1] = v.y;
+        } else {
+          po[i][0] = src[0];
+        }
+      }
+      float nm = mx;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc += __shfl(wl, 2 * i + half, 64) * po[i];
-    mx = nm;
-  }
+      for (int i = 0; i < ROUND; ++i) {
+        if (c0 + i >= ncand) ls[i] = -INFINITY;
+        nm = fmaxf(nm, ls[i]);
+      }
+      if (nm == -INFINITY) continue;           // no key in any partial so far
+      const float keep = exp2f(mx - nm);       // (0 from -inf)
+      wsum *= keep;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], 32, 64);
-  const float inv = wsum > 0.f ? 1.f / wsum : 0.f;
-  if (half == 0 && active) {
-    const floatx4 v = acc * inv;
+      for (int e = 0; e < CH; ++e) acc[e] *= keep;
+#pragma unroll
+      for (int i = 0; i < ROUND; ++i) {
+        const float wl = exp2f(ls[i] - nm);
+        wsum += wl;
+#pragma unroll
+        for (int e = 0; e < CH; ++e) acc[e] = fmaf(wl, po[i][e], acc[e]);
+      }
+      mx = nm;
+    }
+    if constexpr (SPLIT) {
+      __syncthreads();                         // the previous row's values are read
+      part[w][0] = mx;
+      part[w][1] = wsum;
+#pragma unroll
+      for (int e = 0; e < CH; ++e) part[w][2 + lane * CH + e] = acc[e];
+      __syncthreads();
+      if (w != 0) continue;
+      float nm = mx;
+#pragma unroll
+      for (int v = 1; v < 4; ++v) nm = fmaxf(nm, part[v][0]);
+      wsum = 0.f;
+#pragma unroll
+      for (int e = 0; e < CH; ++e) acc[e] = 0.f;
+      if (nm != -INFINITY) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float f = exp2f(part[v][0] - nm);
+          wsum = fmaf(f, part[v][1], wsum);
+#pragma unroll
+          for (int e = 0; e < CH; ++e) acc[e] = fmaf(f, part[v][2 + lane * CH + e], acc[e]);
+        }
+      }
+      mx = nm;
+    }
+    const size_t orow = (size_t)b * rows + row;
+    const float inv = wsum > 0.f ? 1.f / wsum : 0.f;
     if (a.out_bf16) {
-      Pack8 pk;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) pk.b[e] = float_to_bf16(v[e]);
-      *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + orow * D + d4 * 4) = u32x2{pk.u[0], pk.u[1]};
+      __bf16* dst = static_cast<__bf16*>(a.out) + orow * D + lane * CH;
+      if constexpr (CH == 2) {
+        union {
+          __bf16 b[2];
+          uint32_t u;
+        } v;
+        v.b[0] = float_to_bf16(acc[0] * inv);
+        v.b[1] = float_to_bf16(acc[1] * inv);
+        *reinterpret_cast<uint32_t*>(dst) = v.u;
+      } else {
+        dst[0] = float_to_bf16(acc[0] * inv);
+      }
     } else {
-      *reinterpret_cast<floatx4*>(static_cast<float*>(a.out) + orow * D + d4 * 4) = v;
+      float* dst = static_cast<float*>(a.out) + orow * D + lane * CH;
+      if constexpr (CH == 2)
+        *reinterpret_cast<float2*>(dst) = make_float2(acc[0] * inv, acc[1] * inv);
+      else
+        dst[0] = acc[0] * inv;
     }
-  }
-  if (a.lse != nullptr && lane == 0) a.lse[orow] = wsum > 0.f ? (mx + log2f(wsum)) * kLn2 : -INFINITY;
+    if (a.lse != nullptr && lane == 0) a.lse[orow] = wsum > 0.f ? (mx + log2f(wsum)) * kLn2 : -INFINITY;
   }
 }
 
 template <int D, int RB>
-hipError_t launch_wide(const SharedArgs& a, const SharedPlan& p, hipStream_t st) {
+hipError_t launch_bf16(const SharedArgs& a, const SharedPlan& p, hipStream_t st) {
   if (a.out_bf16)
-    hipLaunchKernelGGL((shared_wide_bf16<D, RB, false>), dim3(p.wgs), dim3(512), 0, st, a, p.wgs);
+    hipLaunchKernelGGL((shared_stream_bf16<D, RB, false>), dim3(p.wgs), dim3(512), 0, st, a, p.wgs);
   else
-    hipLaunchKernelGGL((shared_wide_bf16<D, RB, true>), dim3(p.wgs), dim3(512), 0, st, a, p.wgs);
+    hipLaunchKernelGGL((shared_stream_bf16<D, RB, true>), dim3(p.wgs), dim3(512), 0, st, a, p.wgs);
   return hipGetLastError();
 }
 
+template <int ROWS, int TK, int D>
+hipError_t merge_rows(const SharedArgs& a, const SharedPlan& p, hipStream_t st) {
+  const int rows = a.k * a.Hq;
+  if ((long long)a.B * rows <= kSplitRows) {
+    hipLaunchKernelGGL((shared_merge<ROWS, TK, D, true>), dim3((unsigned)(a.B * rows)), dim3(256), 0, st, a, p.wgs, 1,
+                       rows);
+  } else {
+    // about kMergeWaves waves, a whole number of rows each
+    const int per = (int)std::max(1LL, std::min((long long)rows, (long long)a.B * rows / kMergeWaves));
+    const int wgs_seq = (rows + 4 * per - 1) / (4 * per);
+    hipLaunchKernelGGL((shared_merge<ROWS, TK, D, false>), dim3((unsigned)(a.B * (long long)wgs_seq)), dim3(256), 0, st,
+                       a, p.wgs, per, wgs_seq);
+  }
+  return hipGetLastError();
+}
 template <int ROWS, int TK>
 hipError_t launch_merge(const SharedArgs& a, const SharedPlan& p, hipStream_t st) {
-  // about kMergeWaves waves, a whole number of rows each
-  const int rows = a.k * a.Hq;
-  const int per = (int)std::max(1LL, std::min((long long)rows, (long long)a.B * rows / kMergeWaves));
-  const int wgs_seq = (rows + 4 * per - 1) / (4 * per);
-  hipLaunchKernelGGL((shared_merge<ROWS, TK>), dim3((unsigned)(a.B * (long long)wgs_seq)), dim3(256), 0, st, a, p.wgs, per,
-                     wgs_seq);
-  return hipGetLastError();
+  return a.D == 128 ? merge_rows<ROWS, TK, 128>(a, p, st) : merge_rows<ROWS, TK, 64>(a, p, st);
 }
 
 }  // namespace
@@ -915,10 +980,10 @@ hipError_t launch_shared(const SharedArgs& a, const SharedPlan& p, int dtype, hi
     return e != hipSuccess ? e : launch_merge<kRowsF32, kTileF32>(a, p, st);
   }
   if (p.rows_wg == 128) {
-    e = a.D == 128 ? launch_wide<128, 1>(a, p, st) : launch_wide<64, 1>(a, p, st);
+    e = a.D == 128 ? launch_bf16<128, 1>(a, p, st) : launch_bf16<64, 1>(a, p, st);
     return e != hipSuccess ? e : launch_merge<128, kTile>(a, p, st);
   }
-  e = a.D == 128 ? launch_wide<128, 2>(a, p, st) : launch_wide<64, 2>(a, p, st);
+  e = a.D == 128 ? launch_bf16<128, 2>(a, p, st) : launch_bf16<64, 2>(a, p, st);
   return e != hipSuccess ? e : launch_merge<256, kTile>(a, p, st);
 }
 
