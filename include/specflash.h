@@ -654,9 +654,9 @@ int sd_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_strid
  *               is Lmax or 16 * max_pages; its size follows the device as for
  *               sd_verify_attention
  * SD_BF16 with out_dtype SD_F32 feeds the probabilities to the second product
- * as pairs of bf16 (2^-17 of each kept); with out_dtype SD_BF16 as one bf16
- * each (2^-9, the rounding of out itself), a third less matrix work.  SD_F32
- * runs in float64 and gives SD_F32.
+ * as sums of three bf16 (all of their float32 bits); with out_dtype SD_BF16 as
+ * one bf16 each (2^-9, the rounding of out itself), half the matrix work.
+ * SD_F32 runs in float64 and gives SD_F32.
  * Requirements: those of sd_verify_attention for k, Hq, Hkv, D, scale and
  * alignment; 1 <= G <= B; Hq <= 2^16; B k Hq < 2^31; fewer than 2^30 tiles of
  * 32 keys and 16 to 256 rows over all prefixes and sequences at capacity; else

@@ -298,7 +298,8 @@ struct SharedArgs {
   long long own_base;
 };
 
-SharedPlan plan_shared(int B, int k, int Hq, int Hkv, int D, int G, int prefix_cap, int cap, int dtype, int cus);
+SharedPlan plan_shared(int B, int k, int Hq, int Hkv, int D, int G, int prefix_cap, int cap, int dtype, bool out_bf16,
+                       int cus);
 hipError_t launch_shared(const SharedArgs& a, const SharedPlan& p, int dtype, hipStream_t s);
 
 }  // namespace sd

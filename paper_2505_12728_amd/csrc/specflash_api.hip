@@ -855,8 +855,14 @@ size_t sd_verify_shared_workspace_size(int B, int k, int Hq, int Hkv, int D, int
                                        int dtype) {
   int st;
   if (!shared_shape_ok(B, k, Hq, Hkv, D, G, prefix_capacity, capacity, dtype, &st)) return 0;
-  const sd::SharedPlan plan = sd::plan_shared(B, k, Hq, Hkv, D, G, prefix_capacity, capacity, dtype, device_cus());
-  return plan.ok ? plan.workspace_bytes : 0;
+  // enough for either output type
+  size_t most = 0;
+  for (const bool out_bf16 : {false, true}) {
+    const sd::SharedPlan plan =
+        sd::plan_shared(B, k, Hq, Hkv, D, G, prefix_capacity, capacity, dtype, out_bf16, device_cus());
+    if (plan.ok && plan.workspace_bytes > most) most = plan.workspace_bytes;
+  }
+  return most;
 }
 
 int sd_verify_shared(const void* q, const void* k_cache, const void* v_cache, const int32_t* kv_len,
@@ -885,7 +891,8 @@ int sd_verify_shared(const void* q, const void* k_cache, const void* v_cache, co
       !aligned(v_prefix, al) || !aligned(out, out_dtype == SD_BF16 ? 8 : 16) || !aligned(kv_len, 4) ||
       !aligned(prefix_len, 4) || (group_start && !aligned(group_start, 4)) || (lse && !aligned(lse, 4)))
     return SD_ERR_INVALID_ARG;
-  const sd::SharedPlan plan = sd::plan_shared(B, k, Hq, Hkv, D, G, prefix_cap, cap, dtype, device_cus());
+  const sd::SharedPlan plan =
+      sd::plan_shared(B, k, Hq, Hkv, D, G, prefix_cap, cap, dtype, out_dtype == SD_BF16, device_cus());
   if (!plan.ok) return SD_ERR_UNSUPPORTED;
   if (!workspace || workspace_bytes < plan.workspace_bytes || !aligned(workspace, 16)) return SD_ERR_WORKSPACE;
   sd::SharedArgs a{};

@@ -25,9 +25,12 @@
 // Kernel 2 (merge).  One wave per output row finds the partials of its prefix
 //   pair and of its own pair from the same arithmetic and combines them.
 //
-// P is rounded to bf16 for the second product.  fp32 outputs take it as a pair
-// hi + lo (2^-17 of p kept), two products per step; bf16 outputs, rounded to
-// 2^-9 themselves, take hi alone.  The row sums add the fp32 values.
+// P goes into the second product as bf16.  fp32 outputs take it as the sum of
+// three bf16 terms (all 24 bits of p, three products): two would leave 2e-6 of
+// the output, where fp32 products leave 4e-7, and cost 14% less where the matrix
+// cores bound (16 blocks of 6 x 4 rows, 16001 keys: 61 us in two terms, 70 in
+// three).  bf16 outputs, rounded to 2^-9 themselves, take one term.  The row sums
+// add the fp32 values.
 #include <math.h>
 
 #include <algorithm>
@@ -274,7 +277,7 @@ __device__ __forceinline__ void unrolled(F&& f) {
   }
 }
 
-template <int D, int RB, bool HILO>
+template <int D, int RB, int TERMS>
 __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G) {
   constexpr int NW = 8, TK = kTile, NBUF = 4;
   constexpr int DC = D / 32;                   // 32-channel slices (S^T = K Q^T)
@@ -461,7 +464,7 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
     const uint32_t dh = PH >= 0 ? 0u : (uint32_t)(x % NBUF) * HALF;
     const uint32_t dn = PH >= 0 ? 0u : (uint32_t)((x + 1) % NBUF) * HALF;
     constexpr int G0 = NEXT ? 0 : NQK;         // the last tile has no scores to form
-    bf16x8 ph[2][RB], pl[2][RB];
+    bf16x8 p16[TERMS][2][RB];                  // weights as sums of bf16 terms
     floatx4 sn[4][RB];
     float lm[RB];
     auto weights = [&](int kb) {
@@ -474,9 +477,13 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
           if constexpr (MASK) {
             if (t0 + kb * 16 + 4 * G4 + i > lim[rb]) p[i] = 0.f;
           }
-          const __bf16 hi = float_to_bf16(p[i]);
-          ph[kb >> 1][rb][(kb & 1) * 4 + i] = hi;
-          if constexpr (HILO) pl[kb >> 1][rb][(kb & 1) * 4 + i] = float_to_bf16(p[i] - bf16_to_float(hi));
+          float rest = p[i];
+#pragma unroll
+          for (int t = 0; t < TERMS; ++t) {
+            const __bf16 x16 = float_to_bf16(rest);
+            p16[t][kb >> 1][rb][(kb & 1) * 4 + i] = x16;
+            rest -= bf16_to_float(x16);        // exact
+          }
         }
         l[rb] += (p[0] + p[1]) + (p[2] + p[3]);
       }
@@ -507,8 +514,9 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
           vv.u = u32x4{vr[gr & 1][d][0][0], vr[gr & 1][d][0][1], vr[gr & 1][d][1][0], vr[gr & 1][d][1][1]};
 #pragma unroll
           for (int rb = 0; rb < RB; ++rb) {
-            o[rb][4 * pb + d] = mfma_bf16(vv.b, ph[hf][rb], o[rb][4 * pb + d]);
-            if constexpr (HILO) o[rb][4 * pb + d] = mfma_bf16(vv.b, pl[hf][rb], o[rb][4 * pb + d]);
+#pragma unroll
+            for (int t = TERMS - 1; t >= 0; --t)
+              o[rb][4 * pb + d] = mfma_bf16(vv.b, p16[t][hf][rb], o[rb][4 * pb + d]);
           }
         }
         if constexpr (NEXT) {
@@ -902,12 +910,9 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G, int per
   }
 }
 
-template <int D, int RB>
+template <int D, int RB, int TERMS>
 hipError_t launch_bf16(const SharedArgs& a, const SharedPlan& p, hipStream_t st) {
-  if (a.out_bf16)
-    hipLaunchKernelGGL((shared_stream_bf16<D, RB, false>), dim3(p.wgs), dim3(512), 0, st, a, p.wgs);
-  else
-    hipLaunchKernelGGL((shared_stream_bf16<D, RB, true>), dim3(p.wgs), dim3(512), 0, st, a, p.wgs);
+  hipLaunchKernelGGL((shared_stream_bf16<D, RB, TERMS>), dim3(p.wgs), dim3(512), 0, st, a, p.wgs);
   return hipGetLastError();
 }
 
@@ -933,36 +938,36 @@ hipError_t launch_merge(const SharedArgs& a, const SharedPlan& p, hipStream_t st
 
 }  // namespace
 
-SharedPlan plan_shared(int B, int k, int Hq, int Hkv, int D, int G, int prefix_cap, int cap, int dtype, int cus) {
+SharedPlan plan_shared(int B, int k, int Hq, int Hkv, int D, int G, int prefix_cap, int cap, int dtype, bool out_bf16,
+                       int cus) {
   SharedPlan p{};
   const int kg = k * (Hq / Hkv);
   const long long rows = (long long)B * kg;     // of a KV head
   cus = std::max(1, cus);
-  int per_cu;
+  int per_cu = 1;
   if (dtype == 0) {
     p.rows_wg = kRowsF32;
     per_cu = 2;
   } else {
-    // rows of an average group; a wave of two 16-row blocks halves the LDS reads
-    // per product, eight such waves halve the HBM reads per row again
+    // 256 rows halve the copies and LDS reads per row, but a tile of 128 takes
+    // 5/8 of the time of one of 256 (1024 rows, 65500 keys: 340 us in tiles of
+    // 128, 280 in tiles of 256; 384 rows, 16001 keys: 55 and 62), so the places of
+    // the list decide, with groups of average size and every cache at capacity.
+    // fp32 outputs take three terms of P, for which 256 rows leave no registers.
     const long long avg = (rows + G - 1) / G;
-    p.rows_wg = 128;
     auto places = [&](int rows_wg) {
       return Hkv * (G * ((avg + rows_wg - 1) / rows_wg) * ((prefix_cap + kTile - 1) / kTile) +
                     B * (long long)((kg + rows_wg - 1) / rows_wg) * ((cap + kTile - 1) / kTile + start_places(rows_wg)));
     };
-    if (places(256) * 8 <= places(128) * 5) p.rows_wg = 256;
-    per_cu = 1;
+    p.rows_wg = out_bf16 && places(256) * 8 <= places(128) * 5 ? 256 : 128;
   }
+  const int tk = dtype == 0 ? kTileF32 : kTile;
   p.rows_own = std::min((kg + 15) / 16 * 16, p.rows_wg);
-  const int own_tiles = (kg + p.rows_wg - 1) / p.rows_wg;
   const long long prefix_pairs = Hkv * (rows / p.rows_wg + G);
-  const long long own_pairs = (long long)B * Hkv * own_tiles;
-  const int tk = p.rows_wg >= 128 ? kTile : kTileF32;
-  const long long prefix_tiles = prefix_pairs * ((prefix_cap + tk - 1) / tk);
-  const long long own_tiles_cap = own_pairs * ((cap + tk - 1) / tk);
-  p.ok = prefix_tiles + own_tiles_cap + start_places(p.rows_wg) * (prefix_pairs + own_pairs) < (1LL << 30);
-  p.wgs = (int)std::max(1LL, std::min((long long)cus * per_cu, prefix_tiles + own_tiles_cap));
+  const long long own_pairs = (long long)B * Hkv * ((kg + p.rows_wg - 1) / p.rows_wg);
+  const long long tiles = prefix_pairs * ((prefix_cap + tk - 1) / tk) + own_pairs * ((cap + tk - 1) / tk);
+  p.ok = tiles + start_places(p.rows_wg) * (prefix_pairs + own_pairs) < (1LL << 30);
+  p.wgs = (int)std::max(1LL, std::min((long long)cus * per_cu, tiles));
   p.own_base = (prefix_pairs + p.wgs) * p.rows_wg;
   p.part_rows = (size_t)p.own_base + (size_t)(own_pairs + p.wgs) * p.rows_own;
   p.workspace_bytes = p.part_rows * ((size_t)D + 1) * sizeof(float);
@@ -979,12 +984,15 @@ hipError_t launch_shared(const SharedArgs& a, const SharedPlan& p, int dtype, hi
     e = hipGetLastError();
     return e != hipSuccess ? e : launch_merge<kRowsF32, kTileF32>(a, p, st);
   }
-  if (p.rows_wg == 128) {
-    e = a.D == 128 ? launch_bf16<128, 1>(a, p, st) : launch_bf16<64, 1>(a, p, st);
-    return e != hipSuccess ? e : launch_merge<128, kTile>(a, p, st);
+  if (p.rows_wg == 256) {
+    e = a.D == 128 ? launch_bf16<128, 2, 1>(a, p, st) : launch_bf16<64, 2, 1>(a, p, st);
+    return e != hipSuccess ? e : launch_merge<256, kTile>(a, p, st);
   }
-  e = a.D == 128 ? launch_bf16<128, 2>(a, p, st) : launch_bf16<64, 2>(a, p, st);
-  return e != hipSuccess ? e : launch_merge<256, kTile>(a, p, st);
+  if (a.out_bf16)
+    e = a.D == 128 ? launch_bf16<128, 1, 1>(a, p, st) : launch_bf16<64, 1, 1>(a, p, st);
+  else
+    e = a.D == 128 ? launch_bf16<128, 1, 3>(a, p, st) : launch_bf16<64, 1, 3>(a, p, st);
+  return e != hipSuccess ? e : launch_merge<128, kTile>(a, p, st);
 }
 
 }  // namespace sd
