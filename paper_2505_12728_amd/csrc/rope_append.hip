@@ -19,8 +19,11 @@
 // tokens are fewer than the waves the device holds): a lane forms the
 // frequency of its pair once and the sine and cosine once per token, for all
 // heads, and passes them through LDS; then the wave walks the token's heads
-// in units of VE pairs (two 16-byte reads and writes for bf16, VE = 8), with
-// kBatch units of every lane in flight.
+// in units of VE pairs (two 16-byte reads and writes: VE = 8 for bf16, 4 for
+// fp32), with kBatch units of every lane in flight.  Measured: 65536 rows of 80
+// heads of 128 into a cache 527 us, 5.1 TB/s; 6272 rows of 32 heads 18.2 us;
+// 8 rows 3.6 us, the launch and three dependent latencies (a copy of 2 GiB
+// runs at 4.9 TB/s).
 #include <math.h>
 
 #include <algorithm>
@@ -32,7 +35,10 @@ namespace sd {
 namespace {
 
 constexpr int kWavesWg = 4;
-constexpr int kBatch = 4;      // units in flight per lane
+// Units in flight per lane: two leave few enough registers for eight waves a
+// SIMD (26111 rows of a video prompt 104 -> 97 us against four; eight units 148).
+constexpr int kBatch = 2;
+constexpr int kWgsCu = 16;     // work-groups per compute unit, two rounds of those waves
 constexpr double kInv2Pi = 0.15915494309189533577;
 
 // VE values of type T at p as floats, with the widest loads that VE allows
@@ -267,10 +273,11 @@ template <typename TS, typename TD, int VE, bool APPEND>
 hipError_t launch(RopeArgs a, int cus, hipStream_t st) {
   const int units = a.pairs / VE + (a.D - 2 * a.pairs) / VE;
   const long long items = (long long)(a.Hq + 2 * a.Hkv) * units;
-  // waves the device holds at once (8 work-groups per compute unit); while the
-  // tokens are fewer, several waves share a token's heads, a batch each at least
-  const long long waves = (long long)std::max(cus, 1) * 8 * kWavesWg;
-  long long share = std::min(waves / a.T, (items + 64 * kBatch - 1) / (64 * kBatch));
+  // while the tokens are fewer than the grid's waves, several share a token's
+  // heads, down to one unit per lane (8 rows of 32 heads: 5.1 us in one wave each,
+  // 3.6 so)
+  const long long waves = (long long)std::max(cus, 1) * kWgsCu * kWavesWg;
+  long long share = std::min(waves / a.T, (items + 63) / 64);
   a.share = 1;
   while (a.share * 2 <= share && a.share < 64) a.share *= 2;
   a.step_head = (int)(64 * a.share / units);
@@ -285,7 +292,10 @@ hipError_t launch(RopeArgs a, int cus, hipStream_t st) {
 
 template <typename TS, typename TD, bool APPEND>
 hipError_t by_width(const RopeArgs& a, int width, int cus, hipStream_t st) {
-  if (width >= 8) return launch<TS, TD, 8, APPEND>(a, cus, st);
+  // (eight fp32 outputs would be two stores of 16 bytes 32 bytes apart on the
+  // lanes: 20736 rows of 16 heads of 80 51 us, 44 with four)
+  if constexpr (sizeof(TD) == 2)
+    if (width >= 8) return launch<TS, TD, 8, APPEND>(a, cus, st);
   if (width >= 4) return launch<TS, TD, 4, APPEND>(a, cus, st);
   return launch<TS, TD, 1, APPEND>(a, cus, st);
 }
