@@ -185,12 +185,13 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _on_current(*named):
-    """The library launches on the current device: every tensor (name, tensor or
-    None) lies there.  One comparison each; the messages come afterwards."""
+def _on_current(names, *tensors):
+    """The library launches on the current device: every tensor (None: left
+    out) lies there.  One comparison each; the messages come afterwards."""
     c = _torch()._C._cuda_getDevice()
-    for name, t in named:
+    for t in tensors:
         if t is not None and t.get_device() != c:
+            name = names.split()[[x is t for x in tensors].index(True)]
             if not t.is_cuda:
                 raise ValueError(f"{name} must be a GPU tensor")
             raise ValueError(f"{name} must be on cuda:{c}, the current device, got {t.device}")
@@ -856,7 +857,7 @@ def sd_rope(x, pos, theta, sections=None, per_axis=False, inverse=False, out=Non
     one axis, all D / 2).  per_axis restarts the frequencies in every section.
     inverse turns back, which is also the gradient: dx = sd_rope(dy, ...,
     inverse=True).  out may be x (in place).  Returns out [T, H, D]."""
-    _on_current(("x", x), ("pos", pos), ("out", out))
+    _on_current("x pos out", x, pos, out)
     shape, xs = _rows(x, "x")
     T, H, D = shape
     dt = _dtype_code(x)
@@ -887,8 +888,8 @@ def sd_kv_append(q, k, v, k_cache, v_cache, kv_len, theta, pos=None, sections=No
     written in place.  Returns the rotated queries [T, Hq, D] in the cache's
     dtype (None without q)."""
     int32 = _torch().int32
-    _on_current(("q", q), ("k", k), ("v", v), ("k_cache", k_cache), ("v_cache", v_cache), ("kv_len", kv_len),
-                ("pos", pos), ("row_start", row_start), ("page_table", page_table), ("q_out", q_out))
+    _on_current("q k v k_cache v_cache kv_len pos row_start page_table q_out", q, k, v, k_cache, v_cache, kv_len, pos,
+                row_start, page_table, q_out)
     src, dtype = k.dtype, k_cache.dtype
     shape, ks = _rows(k, "k")
     v_shape, vs = _rows(v, "v", src)
@@ -986,9 +987,8 @@ def sd_verify_shared(q, k_cache, v_cache, kv_len, prefix_len, k_prefix=None, v_p
     Returns (out [B, k, Hq, D], lse [B, k, Hq] fp32 or None)."""
     torch = _torch()
     int32, dtype = torch.int32, q.dtype
-    _on_current(("q", q), ("k_cache", k_cache), ("v_cache", v_cache), ("kv_len", kv_len), ("prefix_len", prefix_len),
-                ("k_prefix", k_prefix), ("v_prefix", v_prefix), ("prefix_table", prefix_table),
-                ("group_start", group_start), ("page_table", page_table))
+    _on_current("q k_cache v_cache kv_len prefix_len k_prefix v_prefix prefix_table group_start page_table", q, k_cache,
+                v_cache, kv_len, prefix_len, k_prefix, v_prefix, prefix_table, group_start, page_table)
     _dense(q, "q", dtype, 4)
     _dense(kv_len, "kv_len", int32, 1)
     _dense(prefix_len, "prefix_len", int32, 1)

@@ -13,17 +13,15 @@
 // (bf16), so HBM up to about 300 rows per KV head and the matrix cores beyond.
 //
 // Kernel 1 (stream).  Units are the groups' prefixes, then the sequences' own
-//   caches; a unit's rows in tiles of ROWS and its KV heads give pairs; the
-//   32-key tiles of all pairs form one list, of which each work-group of a
-//   fixed grid takes an equal contiguous range.  Ragged lengths and groups are
-//   balanced to a tile, and lengths and groups are read on the device alone.
-//   Tiles come HBM -> LDS through a ring of global_load_lds copies; a wave
-//   holds RB blocks of 16 rows, so that a fragment read from LDS feeds RB
-//   matrix-core operations:  S^T = K Q^T, online softmax in fp32 (base 2),
-//   O^T += V^T P^T.  Where its range leaves a pair, a work-group writes the
-//   segment's normalised partial (o, lse).
-// Kernel 2 (merge).  One wave per output row finds the partials of its prefix
-//   pair and of its own pair from the same arithmetic and combines them.
+//   caches; a unit's rows in tiles of ROWS and its KV heads give pairs; the key
+//   tiles of all pairs form one list, of which each work-group of a fixed grid
+//   takes an equal contiguous range.  Ragged lengths and groups are balanced to a
+//   tile, and lengths and groups are read on the device alone.  A tile's keys and
+//   values pass through LDS once for all ROWS rows:  S^T = K Q^T, online softmax
+//   in fp32 (base 2), O^T += V^T P^T.  Where its range leaves a pair, a work-group
+//   writes the segment's normalised partial (o, lse).
+// Kernel 2 (merge).  Finds the partials of a row's prefix pair and of its own pair
+//   from the same arithmetic and combines them.
 //
 // P goes into the second product as bf16.  fp32 outputs take it as the sum of
 // three bf16 terms (all 24 bits of p, three products): two would leave 2e-6 of
@@ -31,6 +29,7 @@
 // cores bound (16 blocks of 6 x 4 rows, 16001 keys: 61 us in two terms, 70 in
 // three).  bf16 outputs, rounded to 2^-9 themselves, take one term.  The row sums
 // add the fp32 values.
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -41,15 +40,18 @@
 namespace sd {
 namespace {
 
-
 constexpr int kTileF32 = 32, kTile = 64;   // keys per tile (fp32, bf16)
+constexpr int kRowsF32 = 16;               // rows per work-group (fp32)
 // Places of the list in front of a pair's first tile: on the matrix cores
-// starting a pair (its queries' latency with the ring drained, the partial of
-// the one before) takes about as long as two tiles.
-constexpr int kRowsF32 = 16;
+// starting a pair (its queries' latency, the partial of the one before) takes
+// about as long as two tiles.  Without them the one work-group that got 128
+// one-tile pairs took 502 us where the others took 240 (1024 rows, 65500 keys).
+// One place or three measure within 3% of two.
 constexpr int start_places(int rows_wg) { return rows_wg == kRowsF32 ? 0 : 2; }
-constexpr int kMergeWaves = 8192;   // merge waves take several rows each beyond that many
-constexpr int kSplitRows = 1024;    // and four share a row up to that many
+// Rows in all up to which four merge waves share a row (224 rows: 23.0 us for the
+// call with one wave a row, 17.9 so; 512: 58.6 and 55.8; 1792: 33.2 and 34.6), and
+// waves beyond which each takes several rows.
+constexpr int kSplitRows = 1024, kMergeWaves = 8192;
 constexpr float kHeadroom = 24.f;   // log2 of the largest weight before the maximum is raised
 
 typedef __attribute__((address_space(3))) void lds_void;
@@ -265,6 +267,12 @@ __device__ __forceinline__ int out_row(const SharedArgs& a, int first, int hk, i
 // runs in groups of four LDS fragments: a group's reads are issued one group
 // ahead and waited for by count.  K and V have rings of four slots: a tile's copy
 // has two steps to land.
+//   64 rows over 65500 keys of 8 heads of 128 (268 MB): 50 us, 5.4 TB/s, HBM.
+//   1024 rows there, bf16 out (275 GFLOP): 265 us, 1040 TFLOP/s, where a matrix
+// product of 8192^3 reaches 1346.  Matrix cores busy 49%, no LDS conflicts, clock
+// 2.05 GHz; without the exponentials (in a copy of the kernel) 11% less time,
+// without P V 12%, without the fragment reads 5%, without the copies 2%: no unit
+// binds alone.
 template <int V>
 struct Const {
   static constexpr int value = V;
@@ -452,6 +460,13 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
   auto lane_max = [&](const floatx4& s, float top) {
     return fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), top);
   };
+  // the same over the keys that row block rb may see, s those from key t on: a
+  // masked score that exceeds all visible ones by 2^126 would leave them no weight
+  auto seen_max = [&](floatx4 s, int t, int rb, float top) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = t + i > lim[rb] ? -FLT_MAX : s[i];
+    return lane_max(s, top);
+  };
 
   // One step, tile t0 / TK of the segment at ring step x.  NEXT: there is a tile
   // behind it in the segment.  MASK: a row's last visible key may lie in the tile.
@@ -523,15 +538,19 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
 #pragma unroll
           for (int kb = q * per; kb < (q + 1) * per; ++kb)
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) lm[rb] = lane_max(sn[kb][rb], kb == 0 ? sn[0][rb][0] : lm[rb]);
+            for (int rb = 0; rb < RB; ++rb) {
+              if constexpr (MASK)
+                lm[rb] = seen_max(sn[kb][rb], t0 + TK + kb * 16 + 4 * G4, rb, kb == 0 ? -FLT_MAX : lm[rb]);
+              else
+                lm[rb] = lane_max(sn[kb][rb], kb == 0 ? sn[0][rb][0] : lm[rb]);
+            }
         }
       }
       __builtin_amdgcn_sched_barrier(0);
     });
     if constexpr (NEXT) {
-      // A lane's largest exponent, taken before the mask, bounds the masked ones;
-      // m, raised only where it passes 2^24, may so exceed the true maximum,
-      // which cancels in o = O / l and lse = m + log2 l
+      // m, raised only where an exponent passes 2^24, cancels in o = O / l and
+      // lse = m + log2 l
       bool over = false;
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) over = over || fmaf(lm[rb], sl2, -m[rb]) > kHeadroom;
@@ -590,13 +609,14 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
       });
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        float top = sc[0][rb][0];
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb) top = lane_max(sc[kb][rb], top);
-        m[rb] = wave_max_across_groups(top) * sl2;
-        l[rb] = 0.f;
         const int r = seg.rt * ROWS + (w * RB + rb) * 16 + c;
         lim[rb] = seg.u >= a.G ? seg.L - a.k + r % kg / g : seg.L - 1;
+        float top = -FLT_MAX;
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) top = seen_max(sc[kb][rb], t_first + kb * 16 + 4 * G4, rb, top);
+        top = wave_max_across_groups(top);
+        m[rb] = top == -FLT_MAX ? 0.f : top * sl2;      // 0: no key here, l stays 0
+        l[rb] = 0.f;
 #pragma unroll
         for (int db = 0; db < DB; ++db) o[rb][db] = floatx4{0.f, 0.f, 0.f, 0.f};
       }
@@ -611,20 +631,18 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
       continue;
     }
     int i = 0;                                 // step of the segment
-    // (only the last two tiles of a segment can hold masked keys: k <= 16)
-    for (; i < steps - 2 && x % NBUF != 0; ++i, ++x) step(x, 0, Const<-1>{}, Const<1>{}, Const<0>{});
-    for (; i + NBUF <= steps - 2; i += NBUF, x += NBUF) {
+    // only the last two tiles of a segment can hold masked keys (k <= 16), and the
+    // third from the end forms the scores of the first of them
+    for (; i < steps - 3 && x % NBUF != 0; ++i, ++x) step(x, 0, Const<-1>{}, Const<1>{}, Const<0>{});
+    for (; i + NBUF <= steps - 3; i += NBUF, x += NBUF) {
       step(x, 0, Const<0>{}, Const<1>{}, Const<0>{});
       step(x, 0, Const<1>{}, Const<1>{}, Const<0>{});
       step(x, 0, Const<2>{}, Const<1>{}, Const<0>{});
       step(x, 0, Const<3>{}, Const<1>{}, Const<0>{});
     }
-    for (; i < steps - 2; ++i, ++x) step(x, 0, Const<-1>{}, Const<1>{}, Const<0>{});
-    if (i < steps - 1) {
-      step(x, t_first + i * TK, Const<-1>{}, Const<1>{}, Const<1>{});
-      ++i;
-      ++x;
-    }
+    for (; i < steps - 3; ++i, ++x) step(x, 0, Const<-1>{}, Const<1>{}, Const<0>{});
+#pragma unroll 1
+    for (; i < steps - 1; ++i, ++x) step(x, t_first + i * TK, Const<-1>{}, Const<1>{}, Const<1>{});
     step(x, t_first + i * TK, Const<-1>{}, Const<0>{}, Const<1>{});
     ++x;
 #pragma unroll

@@ -5,7 +5,7 @@ scale in units of 1 / sqrt(D) (inputs N(0, 1)):
   scores     D = 128 fp32 products of sum |q k| scale <= 8 n, summed one after
              the other: 128 * 2^-24 * 8 n = 2^-14 n of each weight, in sum and
              normaliser
-  weights    bf16 pairs keep 2^-16 of each, single bf16 values 2^-8
+  weights    all of their bits in three bf16 terms; single bf16 values 2^-8
   sums       up to 2^9 steps of 32 keys, 2^-24 of A each: 2^-15
 so that 2^-12 max(1, n) A bounds an fp32 output, and 2^-8 (A + |out|) more a
 bf16 one.  fp32 inputs run in float64; their partials and the merge's weights
@@ -158,6 +158,28 @@ def test_shared_rising_scores(rows):
     # scores reach 16 * 12 = 192 from 64 products of one sign: their float32
     # sum is off by at most 64 * 2^-24 * 192, within the bound for n = 8
     check(d, out, lse, reference(d, 1.0), "hilo", 8.0)
+
+
+@pytest.mark.parametrize("k,lens", [(4, [4, 5, 70]), (16, [16, 65, 79, 130]), (2, [1, 2, 66])])
+@pytest.mark.parametrize("rows,prefix", [(64, 0), (256, 8000)])
+def test_shared_masked_keys_weigh_nothing(k, lens, rows, prefix):
+    # the last key, visible to the last block row only, has a score of 512 where
+    # the others have about 0: no other row may know of it, neither where its
+    # tile is a segment's first nor behind one, nor where the block crosses tiles
+    import torch
+    lens = lens * (rows // (k * len(lens)) + 1)
+    d = inputs(lens, [max(prefix, 1)], [len(lens)], k, 1, 1, 64, seed=6)
+    d["prefix_len"][0] = prefix
+    d["q"].fill_(1.0)
+    d["k_prefix"] = (d["k_prefix"].float() / 64).to(torch.bfloat16)
+    for b, n in enumerate(lens):
+        d["k_cache"][b, :n] = (d["k_cache"][b, :n].float() / 64).to(torch.bfloat16)
+        d["k_cache"][b, n - 1] = 8.0
+    ref = reference(d, 1.0)
+    for kind in ("hilo", "bf16"):
+        out, lse = call(d, scale=1.0, out_dtype=torch.bfloat16 if kind == "bf16" else torch.float32)
+        # 512 log2(e) is held to about 2^-14 in the last row's lse
+        check(d, out, lse, ref, kind)
 
 
 def test_shared_equals_verify_where_nothing_is_shared():
