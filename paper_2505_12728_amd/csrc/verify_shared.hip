@@ -631,16 +631,18 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
       continue;
     }
     int i = 0;                                 // step of the segment
-    // only the last two tiles of a segment can hold masked keys (k <= 16), and the
-    // third from the end forms the scores of the first of them
-    for (; i < steps - 3 && x % NBUF != 0; ++i, ++x) step(x, 0, Const<-1>{}, Const<1>{}, Const<0>{});
-    for (; i + NBUF <= steps - 3; i += NBUF, x += NBUF) {
+    // the steps before `open` neither weigh a tile with masked keys nor form the
+    // scores of one
+    const int seen = seg.u >= a.G ? max(seg.L - a.k + 1, 0) : seg.L;   // keys that all rows see
+    const int open = min(seen / TK - 1 - t_first / TK, steps - 1);
+    for (; i < open && x % NBUF != 0; ++i, ++x) step(x, 0, Const<-1>{}, Const<1>{}, Const<0>{});
+    for (; i + NBUF <= open; i += NBUF, x += NBUF) {
       step(x, 0, Const<0>{}, Const<1>{}, Const<0>{});
       step(x, 0, Const<1>{}, Const<1>{}, Const<0>{});
       step(x, 0, Const<2>{}, Const<1>{}, Const<0>{});
       step(x, 0, Const<3>{}, Const<1>{}, Const<0>{});
     }
-    for (; i < steps - 3; ++i, ++x) step(x, 0, Const<-1>{}, Const<1>{}, Const<0>{});
+    for (; i < open; ++i, ++x) step(x, 0, Const<-1>{}, Const<1>{}, Const<0>{});
 #pragma unroll 1
     for (; i < steps - 1; ++i, ++x) step(x, t_first + i * TK, Const<-1>{}, Const<1>{}, Const<1>{});
     step(x, t_first + i * TK, Const<-1>{}, Const<0>{}, Const<1>{});
