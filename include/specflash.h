@@ -591,7 +591,8 @@ int sd_rope(const void* x, int64_t x_stride, const int32_t* pos, void* y, int64_
  *   k, v      [T, Hkv, D] src_dtype, rows every k_stride / v_stride elements
  *             (the three may be views of one fused projection)
  *   q_out     [T, Hq, D] dtype, dense: the rotated queries.  May be q itself
- *             where that is dense and of dtype; else apart from q, k and v
+ *             where that is dense and of dtype; else apart from q, k and v.
+ *             Never a part of the caches
  *   k_cache, v_cache  contiguous (page_table == NULL) [B, Lmax, Hkv, D] dtype,
  *             or page pools [num_pages, Hkv, 16, D], apart from the rows read
  *   row_start [B + 1] int32, not decreasing, or NULL (then B divides T).  Rows
@@ -606,7 +607,7 @@ int sd_rope(const void* x, int64_t x_stride, const int32_t* pos, void* y, int64_
  * A row whose cache position lies outside 0 .. capacity - 1, or whose page id
  * lies outside 0 .. num_pages - 1, is not written to the cache (its q_out is).
  * Two rows never share a cache place unless page_table names a page twice;
- * such a place gets one of the two rows.
+ * each element of such a place is then that of one of the two rows.
  * Requirements: T >= 0 (0 launches nothing), B, Hkv >= 1, Hq >= 0, D <= 256,
  * T <= 2^30, Hq and Hkv <= 2^20, max_pages <= 2^26; src_dtype and dtype equal,
  * or SD_F32 into SD_BF16 (SD_BF16 into SD_F32: SD_ERR_UNSUPPORTED).
@@ -658,9 +659,11 @@ int sd_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_strid
  * one bf16 each (2^-9, the rounding of out itself), half the matrix work.
  * SD_F32 runs in float64 and gives SD_F32.
  * Requirements: those of sd_verify_attention for k, Hq, Hkv, D, scale and
- * alignment; 1 <= G <= B; Hq <= 2^16; B k Hq < 2^31; fewer than 2^30 tiles of
- * 32 keys and 16 to 256 rows over all prefixes and sequences at capacity; else
- * SD_ERR_UNSUPPORTED (the workspace size is then 0).
+ * alignment; 1 <= G <= B <= 2^23; Hq <= 2^16; B k Hq < 2^31; fewer than 2^30
+ * tiles of 32 keys and 16 to 256 rows over all prefixes and sequences at
+ * capacity; else SD_ERR_UNSUPPORTED (the workspace size is then 0).  A key
+ * that is not finite reaches the rows that see it; a value that is not finite
+ * may with SD_BF16 reach every row of its sequence.
  * ---------------------------------------------------------------------- */
 size_t sd_verify_shared_workspace_size(int B, int k, int Hq, int Hkv, int D, int G,
                                        int prefix_capacity, int capacity, int dtype);

@@ -182,6 +182,41 @@ def test_shared_masked_keys_weigh_nothing(k, lens, rows, prefix):
         check(d, out, lse, ref, kind)
 
 
+@pytest.mark.parametrize("kind", ["hilo", "bf16", "f32"])
+def test_shared_nonfinite_keys_reach_the_rows_that_see_them(kind):
+    # the last key of each sequence, and of one the last two: the block rows
+    # before them as without them
+    import torch
+    d = inputs([9, 64, 70, 131], [200], [4], 5, 4, 2, 128, "f32" if kind == "f32" else "bf16", seed=7)
+    out_dtype = torch.bfloat16 if kind == "bf16" else torch.float32
+    ref = reference(d, 1 / math.sqrt(128))
+    want, want_lse = call(d, out_dtype=out_dtype)
+    for b, (n, bad) in enumerate(zip([9, 64, 70, 131], (math.nan, math.inf, -math.inf, math.nan))):
+        d["k_cache"][b, n - 1] = bad
+    d["k_cache"][2, 68] = math.inf
+    out, lse = call(d, out_dtype=out_dtype)
+    for b, rows in enumerate((4, 4, 3, 4)):
+        out[b, rows:], lse[b, rows:] = want[b, rows:], want_lse[b, rows:]
+    check(d, out, lse, ref, kind)
+
+
+def test_shared_two_calls_at_once():
+    # two streams, two workspaces, the same caches: each as it is alone
+    import torch
+    import paper_2505_12728_amd as sd
+    d = inputs([40] * 16, [9000], [16], 8, 8, 2, 128, paged=True, seed=17)
+    dev = {n: torch.as_tensor(d[n]).cuda() for n in d if d[n] is not None}
+    other = dict(dev, q=dev["q"].flip(0).contiguous(), kv_len=(dev["kv_len"] - 7))
+    want = [sd.sd_verify_shared(**a) for a in (dev, other)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(3):
+        got = [sd.sd_verify_shared(**a, stream=s) for _ in range(4) for a, s in zip((dev, other), streams)]
+        torch.cuda.synchronize()
+        for i, (out, lse) in enumerate(got):
+            assert torch.equal(out, want[i % 2][0]) and torch.equal(lse, want[i % 2][1])
+
+
 def test_shared_equals_verify_where_nothing_is_shared():
     import torch
     import paper_2505_12728_amd as sd
