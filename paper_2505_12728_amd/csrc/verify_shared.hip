@@ -42,12 +42,21 @@ namespace {
 
 constexpr int kTileF32 = 32, kTile = 64;   // keys per tile (fp32, bf16)
 constexpr int kRowsF32 = 16;               // rows per work-group (fp32)
-// Places of the list in front of a pair's first tile: on the matrix cores
-// starting a pair (its queries' latency, the partial of the one before) takes
-// about as long as two tiles.  Without them the one work-group that got 128
-// one-tile pairs took 502 us where the others took 240 (1024 rows, 65500 keys).
-// One place or three measure within 3% of two.
-constexpr int start_places(int rows_wg) { return rows_wg == kRowsF32 ? 0 : 2; }
+// Places that the list gives to a tile and to the start of a pair (its queries'
+// latency, the partial of the one before), so that equal ranges take equal times.
+// On the matrix cores, in thirds of a tile whose rows are all there (about 2.2 us):
+// a tile with half of them or fewer takes two (1.4 us with fp32 outputs, 1.3 in
+// tiles of 256 rows), a start six, which one-tile pairs need, whose latencies
+// nothing hides (3.9 us; pairs of 11 tiles 2.2).  Whole tiles for all and two for a
+// start: 96 rows over 700 own keys took 39 us where the prefixes' work-groups took
+// 60 (the call 73.5 us, 70.5 so); three thirds for a start: 1024 rows with 64 own
+// keys 378 us against 330.
+constexpr int kWhole = 3, kStartPlaces = 6;
+constexpr int start_places(int rows_wg) { return rows_wg == kRowsF32 ? 0 : kStartPlaces; }
+constexpr int most_places(int rows_wg) { return rows_wg == kRowsF32 ? 1 : kWhole; }
+__host__ __device__ constexpr int tile_places(int rows_wg, int rows) {   // of a unit of `rows` rows
+  return rows_wg == kRowsF32 ? 1 : 2 * rows <= rows_wg ? 2 : kWhole;
+}
 // Rows in all up to which four merge waves share a row (224 rows: 23.0 us for the
 // call with one wave a row, 17.9 so; 512: 58.6 and 55.8; 1792: 33.2 and 34.6), and
 // waves beyond which each takes several rows.
@@ -96,6 +105,7 @@ struct Cursor {
   int u;             // unit
   int hk, rt, t;     // KV head, row tile, key tile
   int nt, RT;        // key tiles and row tiles of the unit
+  int wt;            // places of one of its tiles
   int L, rows, first, end;
   int pair;          // pairs of the same kind (prefix or own) before this one
 };
@@ -140,7 +150,7 @@ __device__ __forceinline__ Span scan_units(const SharedArgs& a, int u0, Carry& c
   }
   c.bound = max(c.bound, last_lane(bound));
   s.pairs = a.Hkv * row_tiles(s.un.rows, ROWS);
-  s.places = s.un.L > 0 ? s.pairs * (tiles_of<TK>(s.un.L) + start_places(ROWS)) : 0;
+  s.places = s.un.L > 0 ? s.pairs * (tiles_of<TK>(s.un.L) * tile_places(ROWS, s.un.rows) + start_places(ROWS)) : 0;
   auto add = [](int x, int y) { return x + y; };
   const int ti = wave_scan(s.places, add), pi = wave_scan(s.pairs, add);
   s.n_before = c.places + ti - s.places;
@@ -150,8 +160,48 @@ __device__ __forceinline__ Span scan_units(const SharedArgs& a, int u0, Carry& c
   return s;
 }
 
-// cursor of the first tile at place n or behind it, from the span that holds
-// place n.  The pair counts its kind only: own pairs start at 0 again.
+// place of the tile behind cu
+template <int ROWS>
+__device__ __forceinline__ int place_behind(const Cursor& cu) {
+  return cu.n + cu.wt + (cu.t + 1 == cu.nt ? start_places(ROWS) : 0);
+}
+
+// next tile of the list; behind the last one a place past the list
+template <int ROWS, int TK>
+__device__ __forceinline__ void advance(const SharedArgs& a, Cursor& cu) {
+  cu.n += cu.wt;
+  if (++cu.t < cu.nt) return;
+  cu.t = 0;
+  cu.n += start_places(ROWS);
+  ++cu.pair;
+  if (++cu.rt < cu.RT) return;
+  cu.rt = 0;
+  if (++cu.hk < a.Hkv) return;
+  cu.hk = 0;
+  do {
+    ++cu.u;
+    if (cu.u < a.G) {
+      cu.first = cu.end;
+      cu.end = max(cu.end, group_bound(a, cu.u + 1));
+      cu.rows = (cu.end - cu.first) * a.k * (a.Hq / a.Hkv);
+      cu.L = min(max(((cint32*)a.prefix_len)[cu.u], 0), a.prefix_cap);
+    } else {
+      if (cu.u == a.G) cu.pair = 0;
+      cu.first = cu.u - a.G;
+      cu.end = cu.first + 1;
+      cu.rows = a.k * (a.Hq / a.Hkv);
+      cu.L = cu.first < a.B ? min(max(((cint32*)a.kv_len)[cu.first], 0), a.cap) : 0;
+    }
+    cu.nt = tiles_of<TK>(cu.L);
+    cu.RT = row_tiles(cu.rows, ROWS);
+    cu.wt = tile_places(ROWS, cu.rows);
+    if (cu.nt == 0 || cu.RT == 0) cu.pair += a.Hkv * cu.RT;
+  } while ((cu.nt == 0 || cu.RT == 0) && cu.u < a.G + a.B);
+}
+
+// Cursor of the first tile at place n or behind it (a tile's place is its first),
+// from the span that holds place n; behind the list's last tile that is a place
+// past the list.  The pair counts its kind only: own pairs start at 0 again.
 template <int ROWS, int TK>
 __device__ __forceinline__ Cursor tile_in(const SharedArgs& a, const Span& s, int u0, int n) {
   constexpr int kStart = start_places(ROWS);
@@ -165,13 +215,16 @@ __device__ __forceinline__ Cursor tile_in(const SharedArgs& a, const Span& s, in
   cu.end = of(s.un.end);
   cu.nt = tiles_of<TK>(cu.L);
   cu.RT = row_tiles(cu.rows, ROWS);
-  const int rem = n - of(s.n_before);
-  const int x = rem / (cu.nt + kStart);
-  cu.t = max(rem - x * (cu.nt + kStart) - kStart, 0);
-  cu.n = of(s.n_before) + x * (cu.nt + kStart) + kStart + cu.t;
+  cu.wt = tile_places(ROWS, cu.rows);
+  const int rem = n - of(s.n_before), len = cu.nt * cu.wt + kStart;
+  const int x = rem / len;
+  const int t = (max(rem - x * len - kStart, 0) + cu.wt - 1) / cu.wt;
+  cu.t = min(t, cu.nt - 1);
+  cu.n = of(s.n_before) + x * len + kStart + cu.t * cu.wt;
   cu.hk = x / cu.RT;
   cu.rt = x - cu.hk * cu.RT;
   cu.pair = cu.u < a.G ? of(s.p_before) + x : (cu.u - a.G) * a.Hkv * cu.RT + x;
+  if (t == cu.nt) advance<ROWS, TK>(a, cu);    // n lies inside the pair's last tile
   return cu;
 }
 
@@ -199,50 +252,12 @@ __device__ __forceinline__ bool first_tile(const SharedArgs& a, int w, int G, Cu
       break;
     }
   }
-  int* f[] = {&cu.n, &cu.u, &cu.hk, &cu.rt, &cu.t, &cu.nt, &cu.RT, &cu.L, &cu.rows, &cu.first, &cu.end, &cu.pair};
+  int* f[] = {&cu.n, &cu.u, &cu.hk, &cu.rt, &cu.t, &cu.nt, &cu.RT, &cu.wt, &cu.L, &cu.rows, &cu.first, &cu.end, &cu.pair};
 #pragma unroll
   for (int* x : f) *x = __builtin_amdgcn_readfirstlane(*x);
   *first = cu;
   *behind = n1;
   return cu.n < n1;
-}
-
-// place of the tile behind cu
-template <int ROWS>
-__device__ __forceinline__ int place_behind(const Cursor& cu) {
-  return cu.n + 1 + (cu.t + 1 == cu.nt ? start_places(ROWS) : 0);
-}
-
-// next tile of the list; the caller never steps past the last one
-template <int ROWS, int TK>
-__device__ __forceinline__ void advance(const SharedArgs& a, Cursor& cu) {
-  ++cu.n;
-  if (++cu.t < cu.nt) return;
-  cu.t = 0;
-  cu.n += start_places(ROWS);
-  ++cu.pair;
-  if (++cu.rt < cu.RT) return;
-  cu.rt = 0;
-  if (++cu.hk < a.Hkv) return;
-  cu.hk = 0;
-  do {
-    ++cu.u;
-    if (cu.u < a.G) {
-      cu.first = cu.end;
-      cu.end = max(cu.end, group_bound(a, cu.u + 1));
-      cu.rows = (cu.end - cu.first) * a.k * (a.Hq / a.Hkv);
-      cu.L = min(max(((cint32*)a.prefix_len)[cu.u], 0), a.prefix_cap);
-    } else {
-      if (cu.u == a.G) cu.pair = 0;
-      cu.first = cu.u - a.G;
-      cu.end = cu.first + 1;
-      cu.rows = a.k * (a.Hq / a.Hkv);
-      cu.L = cu.first < a.B ? min(max(((cint32*)a.kv_len)[cu.first], 0), a.cap) : 0;
-    }
-    cu.nt = tiles_of<TK>(cu.L);
-    cu.RT = row_tiles(cu.rows, ROWS);
-    if (cu.nt == 0 || cu.RT == 0) cu.pair += a.Hkv * cu.RT;
-  } while ((cu.nt == 0 || cu.RT == 0) && cu.u < a.G + a.B);
 }
 
 // First row of the partial that work-group w writes for the pair of cursor cu:
@@ -579,11 +594,11 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
   for (int i = 0; i < NBUF - 1; ++i) copy_next(i);
   int x = 0;                                   // ring step
   while (true) {
-    const int steps = min(cc.nt - cc.t, n1 - cc.n);
+    const int steps = min(cc.nt - cc.t, (n1 - cc.n + cc.wt - 1) / cc.wt);
     const int t_first = cc.t * TK;
     const Cursor seg = cc;
     cc.t += steps - 1;
-    cc.n += steps - 1;
+    cc.n += (steps - 1) * cc.wt;
     const bool more = place_behind<ROWS>(cc) < n1;
     if (more) advance<ROWS, TK>(a, cc);        // the next segment
     if (x == 0) wait_vm_then_barrier<2 * TILE_COPIES>();   // the first tile has landed
@@ -772,9 +787,9 @@ __global__ __launch_bounds__(256) void shared_stream_f32(SharedArgs a, int G) {
 }
 
 // ------------------------------------------------------------------ merge
-// The tiles at places [U, U + nt) of a pair lie with work-groups owner(U) ..
-// owner(U + nt - 1), owner(n) = floor(((n + 1) G - 1) / T), each of which wrote
-// one partial (with fewer places than work-groups, each owner did).  A row's
+// The tiles at places U, U + wt .. of a pair lie with work-groups owner(U) ..
+// owner(U + (nt - 1) wt), owner(n) = floor(((n + 1) G - 1) / T), each of which
+// wrote one partial (with few places, the owners of its tiles did).  A row's
 // candidates are the partials of its prefix pair, then of its own pair.  A wave
 // holds the row's channels (D / 64 per lane) and takes 8 candidates at a time:
 // their lse are the same on every lane, so that their weights 2^(lse - max) need
@@ -794,7 +809,7 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G, int per
 
   // places before the unit, key tiles, pairs before it, row tiles and first row
   // of the sequence, for the group's prefix (0) and the sequence's own keys (1)
-  int before[2] = {0, 0}, nt[2] = {0, 0}, pairs[2] = {0, 0}, RT[2] = {1, 1}, base[2] = {0, 0};
+  int before[2] = {0, 0}, nt[2] = {0, 0}, wt[2] = {1, 1}, pairs[2] = {0, 0}, RT[2] = {1, 1}, base[2] = {0, 0};
   Carry c;
   for (int u0 = 0; u0 < a.G + a.B; u0 += 64) {
     const Span s = scan_units<ROWS, TK>(a, u0, c);
@@ -807,6 +822,7 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G, int per
       const int f = __builtin_ctzll(hit);
       auto of = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
       RT[kind] = row_tiles(of(s.un.rows), ROWS);
+      wt[kind] = tile_places(ROWS, of(s.un.rows));
       nt[kind] = tiles_of<TK>(of(s.un.L));
       before[kind] = of(s.n_before);
       pairs[kind] = kind == 0 ? of(s.p_before) : b * a.Hkv * RT[kind];
@@ -814,7 +830,9 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G, int per
     }
   }
   const int T = c.places;
-  const bool sparse = T < G;   // then a work-group has one place or none: a candidate per tile
+  // with fewer places than the work-groups need for a tile each, some between
+  // two owners may have none: a candidate per tile, each owner's first one counts
+  const bool sparse = T < G * most_places(ROWS);
   // ((n + 1) G - 1) / T: the float64 quotient is off by less than one
   const double inv_t = 1.0 / (double)max(T, 1);
   auto owner = [&](int n) {
@@ -831,11 +849,11 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G, int per
     for (int kind = 0; kind < 2; ++kind) {
       const int r = base[kind] + j * g + (h - hk * g);
       const int x = hk * RT[kind] + r / ROWS;
-      U[kind] = before[kind] + x * (nt[kind] + start_places(ROWS)) + start_places(ROWS);
+      U[kind] = before[kind] + x * (nt[kind] * wt[kind] + start_places(ROWS)) + start_places(ROWS);
       first[kind] = (long long)part_row<ROWS>(a, kind == 1, pairs[kind] + x, 0) + r % ROWS;
       if (nt[kind] == 0) continue;
       wf[kind] = owner(U[kind]);
-      nc[kind] = sparse ? nt[kind] : owner(U[kind] + nt[kind] - 1) - wf[kind] + 1;
+      nc[kind] = sparse ? nt[kind] : owner(U[kind] + (nt[kind] - 1) * wt[kind]) - wf[kind] + 1;
     }
     const int ncand = nc[0] + nc[1];
     float mx = -INFINITY, wsum = 0.f, acc[CH];
@@ -847,9 +865,10 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G, int per
       for (int i = 0; i < ROUND; ++i) {
         const int cand = min(c0 + i, ncand - 1);
         const int kind = cand >= nc[0], k = cand - (kind ? nc[0] : 0);
-        const int wv = sparse ? owner(U[kind] + k) : wf[kind] + k;
+        const int wv = sparse ? owner(U[kind] + k * wt[kind]) : wf[kind] + k;
         const size_t prow = (size_t)(first[kind] + (long long)wv * (kind ? a.rows_own : ROWS));
         ls[i] = a.part_lse[prow];
+        if (sparse && k > 0 && owner(U[kind] + (k - 1) * wt[kind]) == wv) ls[i] = -INFINITY;
         const float* src = a.part_o + prow * D + lane * CH;
         if constexpr (CH == 2) {
           const float2 v = *reinterpret_cast<const float2*>(src);
@@ -976,8 +995,12 @@ SharedPlan plan_shared(int B, int k, int Hq, int Hkv, int D, int G, int prefix_c
     // fp32 outputs take three terms of P, for which 256 rows leave no registers.
     const long long avg = (rows + G - 1) / G;
     auto places = [&](int rows_wg) {
-      return Hkv * (G * ((avg + rows_wg - 1) / rows_wg) * ((prefix_cap + kTile - 1) / kTile) +
-                    B * (long long)((kg + rows_wg - 1) / rows_wg) * ((cap + kTile - 1) / kTile + start_places(rows_wg)));
+      auto of = [&](long long pairs, long long unit_rows, int keys) {
+        return pairs * ((long long)((keys + kTile - 1) / kTile) *
+                            tile_places(rows_wg, (int)std::min(unit_rows, (long long)rows_wg)) + start_places(rows_wg));
+      };
+      return Hkv * (of(G * ((avg + rows_wg - 1) / rows_wg), avg, prefix_cap) +
+                    of(B * (long long)((kg + rows_wg - 1) / rows_wg), kg, cap));
     };
     p.rows_wg = out_bf16 && places(256) * 8 <= places(128) * 5 ? 256 : 128;
   }
@@ -986,7 +1009,7 @@ SharedPlan plan_shared(int B, int k, int Hq, int Hkv, int D, int G, int prefix_c
   const long long prefix_pairs = Hkv * (rows / p.rows_wg + G);
   const long long own_pairs = (long long)B * Hkv * ((kg + p.rows_wg - 1) / p.rows_wg);
   const long long tiles = prefix_pairs * ((prefix_cap + tk - 1) / tk) + own_pairs * ((cap + tk - 1) / tk);
-  p.ok = tiles + start_places(p.rows_wg) * (prefix_pairs + own_pairs) < (1LL << 30);
+  p.ok = tiles < (1LL << 27);   // a pair has a tile or more: at most 9 places for each
   p.wgs = (int)std::max(1LL, std::min((long long)cus * per_cu, tiles));
   p.own_base = (prefix_pairs + p.wgs) * p.rows_wg;
   p.part_rows = (size_t)p.own_base + (size_t)(own_pairs + p.wgs) * p.rows_own;
