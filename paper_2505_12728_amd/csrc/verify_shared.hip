@@ -48,8 +48,8 @@ constexpr int kRowsF32 = 16;               // rows per work-group (fp32)
 // a tile with half of them or fewer takes two (1.4 us with fp32 outputs, 1.3 in
 // tiles of 256 rows), a start six, which one-tile pairs need, whose latencies
 // nothing hides (3.9 us; pairs of 11 tiles 2.2).  Whole tiles for all and two for a
-// start: 96 rows over 700 own keys took 39 us where the prefixes' work-groups took
-// 60 (the call 73.5 us, 70.5 so); three thirds for a start: 1024 rows with 64 own
+// start: own caches of 24 rows and 700 keys took 39 us where the prefixes' work-groups
+// took 60 (the call 73.5 us, 70.5 so); three thirds for a start: 1024 rows with 64 own
 // keys 378 us against 330.
 constexpr int kWhole = 3, kStartPlaces = 6;
 constexpr int start_places(int rows_wg) { return rows_wg == kRowsF32 ? 0 : kStartPlaces; }
@@ -688,8 +688,8 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
 // maximum and sum go over those lanes by shuffles, and each accumulates D / 16
 // of its channels.  A tile is a chain of latencies (load 2.0 us, scores 2.5,
 // softmax 0.5, P V 3.2 at 64 channels), which more loads in flight and values
-// read whether they weigh or not shorten: 96 rows of 8 heads of 128 over 4300 keys
-// 1145 us without them, 721 so.
+// read whether they weigh or not shorten: 384 rows of each of 8 KV heads of 128
+// over 4000 keys 1145 us without them, 721 so.
 template <int D>
 __global__ __launch_bounds__(256) void shared_stream_f32(SharedArgs a, int G) {
   constexpr int TK = kTileF32, R = kRowsF32, DS = D + 1;
