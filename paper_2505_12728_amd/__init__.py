@@ -232,21 +232,22 @@ def _workspace(nbytes, device, given):
     return torch.zeros(nbytes, dtype=torch.uint8, device=device), nbytes
 
 
-def _empty(shape, dtype, device, stream):
+def _empty(shape, strides, dtype, device, stream):
     """Memory for a call on `stream`: a given stream's own, so that the
-    allocator reuses it behind that stream's work."""
+    allocator reuses it behind that stream's work.  Plain tuples: 1.3 us, where
+    torch.empty takes 1.7, and 2.3 from a torch.Size."""
     torch = _torch()
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty_strided(shape, strides, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty_strided(shape, strides, dtype=dtype, device=device)
 
 
 def _scratch(nbytes, device, given, stream):
     """_workspace for calls that keep no counters in it: left as allocated."""
     if given is not None or nbytes == 0:
         return _workspace(nbytes, device, given)
-    return _empty(nbytes, _torch().uint8, device, stream), nbytes
+    return _empty((nbytes,), (1,), _torch().uint8, device, stream), nbytes
 
 
 def _raise(status, where):
@@ -863,8 +864,8 @@ def sd_rope(x, pos, theta, sections=None, per_axis=False, inverse=False, out=Non
     dt = _dtype_code(x)
     axes, secs = _axes(pos, sections, T)
     if out is None:
-        out = _empty(shape, x.dtype, x.device, stream)
         ys = H * D
+        out = _empty((T, H, D), (ys, D, 1), x.dtype, x.device, stream)
     else:
         out_shape, ys = _rows(out, "out", x.dtype)
         if out_shape != shape:
@@ -927,7 +928,7 @@ def sd_kv_append(q, k, v, k_cache, v_cache, kv_len, theta, pos=None, sections=No
         if q_shape[0] != T or q_shape[2] != D:
             raise ValueError("q must be [T, Hq, D] with the rows of k")
         if q_out is None:
-            q_out = _empty(q_shape, dtype, k.device, stream)
+            q_out = _empty((T, Hq, D), (Hq * D, D, 1), dtype, k.device, stream)
         else:
             _out(q_out, "q_out", (T, Hq, D), dtype, k.device)
         qp, qop = q.data_ptr(), q_out.data_ptr()
@@ -1025,12 +1026,12 @@ def sd_verify_shared(q, k_cache, v_cache, kv_len, prefix_len, k_prefix=None, v_p
         raise TypeError(f"unsupported out_dtype {out_dtype}: use float32 or bfloat16")
     dev = q.device
     if out is None:
-        out = _empty(shape, out_dtype, dev, stream)
+        out = _empty((B, k, Hq, D), (k * Hq * D, Hq * D, D, 1), out_dtype, dev, stream)
     else:
         _out(out, "out", shape, out_dtype, dev)
     lse_t = None
     if lse is True:
-        lse_t = _empty(shape[:3], torch.float32, dev, stream)
+        lse_t = _empty((B, k, Hq), (k * Hq, Hq, 1), torch.float32, dev, stream)
     elif lse is not None and lse is not False:
         lse_t = _out(lse, "lse", shape[:3], torch.float32, dev)
     lib = library()
