@@ -45,7 +45,7 @@ from .lm_head import lm_head_logits, softmax_temperature, lm_head_probs, sample_
 from .accept_logits import philox4x64, philox_uniforms, spec_accept_logits
 from .draft_layer import (rms_norm, rope, linear, silu, swiglu, semi_ar_layer, semi_ar_draft, bf16_round,
                           dequantize_rows, linear_q8, semi_ar_layer_q8)
-from .rope import rope_angles, rope_axes, append_places, kv_append
+from .rotary import rope_angles, rope_axes, append_places, kv_append
 from .accept import (
     spec_accept,
     spec_accept_one,
