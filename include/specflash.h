@@ -659,7 +659,7 @@ int sd_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_strid
  * one bf16 each (2^-9, the rounding of out itself), half the matrix work.
  * SD_F32 runs in float64 and gives SD_F32.
  * Requirements: those of sd_verify_attention for k, Hq, Hkv, D, scale and
- * alignment; 1 <= G <= B <= 2^23; Hq <= 2^16; B k Hq < 2^31; fewer than 2^27
+ * alignment; 1 <= G <= B <= 2^16; Hq <= 2^16; B k Hq < 2^31; fewer than 2^27
  * tiles of 32 keys and 16 to 256 rows over all prefixes and sequences at
  * capacity; else SD_ERR_UNSUPPORTED (the workspace size is then 0).  A key
  * that is not finite reaches the rows that see it; a value that is not finite

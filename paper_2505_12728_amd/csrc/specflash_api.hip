@@ -846,8 +846,8 @@ static bool shared_shape_ok(int B, int k, int Hq, int Hkv, int D, int G, int pre
   *status = SD_ERR_INVALID_ARG;
   if (G < 1 || prefix_cap < 1 || cap < 1) return false;
   *status = SD_ERR_UNSUPPORTED;
-  // (the merge's grid has a work-group of 256 per sequence: B < 2^24)
-  if (G > B || B > (1 << 23) || Hq > (1 << 16) || (long long)B * k * Hq >= (1LL << 31)) return false;
+  // (every merge wave scans the units: B^2 in all)
+  if (G > B || B > (1 << 16) || Hq > (1 << 16) || (long long)B * k * Hq >= (1LL << 31)) return false;
   *status = SD_OK;
   return true;
 }

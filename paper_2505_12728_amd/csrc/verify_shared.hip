@@ -668,11 +668,11 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
       const int lr = (w * RB + rb) * 16 + c;
       if (seg.rt * ROWS + lr >= seg.rows) continue;
       const size_t prow = part_row<ROWS>(a, seg.u >= a.G, seg.pair, wg) + lr;
-      const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+      const float inv = lsum != 0.f ? 1.f / lsum : 0.f;   // (a NaN stays one)
 #pragma unroll
       for (int db = 0; db < DB; ++db)
         *reinterpret_cast<floatx4*>(a.part_o + prow * D + db * 16 + 4 * G4) = o[rb][db] * inv;
-      if (G4 == 0) a.part_lse[prow] = lsum > 0.f ? m[rb] + log2f(lsum) : -INFINITY;
+      if (G4 == 0) a.part_lse[prow] = lsum != 0.f ? m[rb] + log2f(lsum) : -INFINITY;
     }
     if (!more) break;
     busy = load_rows(cc);
@@ -795,8 +795,8 @@ __global__ __launch_bounds__(256) void shared_stream_f32(SharedArgs a, int G) {
     if ((fresh || end) && row < cu.rows) {
       const size_t at = part_row<R>(a, own, cu.pair, wg) + r;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) a.part_o[at * D + lane16 + 16 * e] = l > 0.0 ? (float)(o[e] / l) : 0.f;
-      if (lane16 == 0) a.part_lse[at] = l > 0.0 ? (float)((m + log(l)) * 1.4426950408889634) : -INFINITY;
+      for (int e = 0; e < PER; ++e) a.part_o[at * D + lane16 + 16 * e] = l != 0.0 ? (float)(o[e] / l) : 0.f;
+      if (lane16 == 0) a.part_lse[at] = l != 0.0 ? (float)((m + log(l)) * 1.4426950408889634) : -INFINITY;
     }
     if (end) break;
     advance<R, TK>(a, cu);
@@ -896,12 +896,14 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G, int per
         }
       }
       float nm = mx;
+      bool none = mx == -INFINITY;
 #pragma unroll
       for (int i = 0; i < ROUND; ++i) {
         if (c0 + i >= ncand) ls[i] = -INFINITY;
         nm = fmaxf(nm, ls[i]);
+        none = none && ls[i] == -INFINITY;
       }
-      if (nm == -INFINITY) continue;           // no key in any partial so far
+      if (none) continue;                      // no key in any partial so far
       const float keep = exp2f(mx - nm);       // (0 from -inf)
       wsum *= keep;
 #pragma unroll
@@ -929,19 +931,17 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G, int per
       wsum = 0.f;
 #pragma unroll
       for (int e = 0; e < CH; ++e) acc[e] = 0.f;
-      if (nm != -INFINITY) {
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const float f = exp2f(part[v][0] - nm);
-          wsum = fmaf(f, part[v][1], wsum);
+      for (int v = 0; v < 4; ++v) {
+        const float f = part[v][0] == nm ? 1.f : exp2f(part[v][0] - nm);   // (-inf too)
+        wsum = fmaf(f, part[v][1], wsum);
 #pragma unroll
-          for (int e = 0; e < CH; ++e) acc[e] = fmaf(f, part[v][2 + lane * CH + e], acc[e]);
-        }
+        for (int e = 0; e < CH; ++e) acc[e] = fmaf(f, part[v][2 + lane * CH + e], acc[e]);
       }
       mx = nm;
     }
     const size_t orow = (size_t)b * rows + row;
-    const float inv = wsum > 0.f ? 1.f / wsum : 0.f;
+    const float inv = wsum != 0.f ? 1.f / wsum : 0.f;
     if (a.out_bf16) {
       __bf16* dst = static_cast<__bf16*>(a.out) + orow * D + lane * CH;
       if constexpr (CH == 2) {
@@ -962,7 +962,7 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G, int per
       else
         dst[0] = acc[0] * inv;
     }
-    if (a.lse != nullptr && lane == 0) a.lse[orow] = wsum > 0.f ? (mx + log2f(wsum)) * kLn2 : -INFINITY;
+    if (a.lse != nullptr && lane == 0) a.lse[orow] = wsum != 0.f ? (mx + log2f(wsum)) * kLn2 : -INFINITY;
   }
 }
 

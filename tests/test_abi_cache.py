@@ -131,10 +131,9 @@ def test_shared_unsupported(shared, lib):
                 dict(B=1 << 20, G=1 << 20, lmax=1 << 20), dict(B=1 << 28, Hq=8, Hkv=8, G=1),
                 dict(Hq=1 << 17, Hkv=1 << 17)):
         assert shared(**bad) == sd.SD_ERR_UNSUPPORTED, bad
-    # more sequences than the merge's grid takes
-    assert shared(B=(1 << 23) + 1, k=1, Hq=1, Hkv=1, G=1) == sd.SD_ERR_UNSUPPORTED
-    assert lib.sd_verify_shared_workspace_size((1 << 23) + 1, 1, 1, 1, 64, 1, 1, 1, 1) == 0
-    assert lib.sd_verify_shared_workspace_size(1 << 23, 1, 1, 1, 64, 1, 1, 1, 1) > 0
+    assert shared(B=(1 << 16) + 1, k=1, Hq=1, Hkv=1, G=1) == sd.SD_ERR_UNSUPPORTED
+    assert lib.sd_verify_shared_workspace_size((1 << 16) + 1, 1, 1, 1, 64, 1, 1, 1, 1) == 0
+    assert lib.sd_verify_shared_workspace_size(1 << 16, 1, 1, 1, 64, 1, 1, 1, 1) > 0
     assert lib.sd_verify_shared_workspace_size(1 << 20, 4, 8, 2, 128, 1, 64, 1 << 20, 1) == 0
     assert lib.sd_verify_shared_workspace_size(4, 4, 8, 2, 128, 5, 64, 64, 1) == 0
     assert lib.sd_verify_shared_workspace_size(4, 4, 8, 2, 128, 4, 64, 64, 1) > 0

@@ -200,6 +200,43 @@ def test_shared_nonfinite_keys_reach_the_rows_that_see_them(kind):
     check(d, out, lse, ref, kind)
 
 
+@pytest.mark.parametrize("kind", ["hilo", "bf16", "f32"])
+@pytest.mark.parametrize("B", [3, 300])
+def test_shared_nan_rows_stay_nan(kind, B):
+    # a query that is not a number, and a row whose only own key is none: those
+    # rows alone, in out and lse
+    import torch
+    d = inputs([40] * B, [90], [B], 2, 4, 2, 64, "f32" if kind == "f32" else "bf16", seed=8)
+    out_dtype = torch.bfloat16 if kind == "bf16" else torch.float32
+    ref = reference(d, 1 / 8)
+    want, want_lse = call(d, out_dtype=out_dtype)
+    d["q"][1, 0, 3, 5] = math.nan
+    d["k_cache"][2, 39, 1] = math.nan              # the last block row of heads 2 and 3
+    out, lse = call(d, out_dtype=out_dtype)
+    for at in ((1, 0, slice(3, 4)), (2, 1, slice(2, 4))):
+        assert bool(torch.isnan(out[at]).all()) and bool(torch.isnan(lse[at]).all())
+        out[at], lse[at] = want[at], want_lse[at]
+    check(d, out, lse, ref, kind)
+
+
+def test_shared_most_sequences():
+    # the largest batch, each sequence with a prefix of its own: two keys a row
+    import torch
+    import paper_2505_12728_amd as sd
+    B, D = 1 << 16, 64
+    g = torch.Generator(device="cuda").manual_seed(18)
+    rnd = lambda: torch.randn(B, 1, 1, D, generator=g, device="cuda").to(torch.bfloat16)     # noqa: E731
+    q, k, v, kp, vp = (rnd() for _ in range(5))
+    one = torch.ones(B, dtype=torch.int32, device="cuda")
+    out, lse = sd.sd_verify_shared(q, k, v, one, one, k_prefix=kp, v_prefix=vp)
+    s = torch.stack([(q.double() * x.double()).sum(-1) / 8 for x in (k, kp)])
+    w = torch.softmax(s, 0)[..., None]
+    want = w[0] * v.double() + w[1] * vp.double()
+    A = w[0] * v.double().abs() + w[1] * vp.double().abs()
+    assert bool(((out - want).abs() <= 2.0 ** -12 * A).all())
+    assert bool(((lse - torch.logsumexp(s, 0)).abs() <= 2.0 ** -12).all())
+
+
 def test_shared_two_calls_at_once():
     # two streams, two workspaces, the same caches: each as it is alone
     import torch
