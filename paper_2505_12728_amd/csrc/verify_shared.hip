@@ -24,10 +24,10 @@
 //   from the same arithmetic and combines them.
 //
 // P goes into the second product as bf16.  fp32 outputs take it as the sum of
-// three bf16 terms (all 24 bits of p, three products): two would leave 2e-6 of
-// the output, where fp32 products leave 4e-7, and cost 14% less where the matrix
-// cores bound (16 blocks of 6 x 4 rows, 16001 keys: 61 us in two terms, 70 in
-// three).  bf16 outputs, rounded to 2^-9 themselves, take one term.  The row sums
+// three bf16 terms (all 24 bits of p, eight each, three products): two would leave
+// 2e-6 of the output, where fp32 products leave 4e-7, and cost 14% less where the
+// matrix cores bound (16 blocks of 6 x 4 rows, 16001 keys: 61 us in two terms, 70
+// in three).  bf16 outputs, rounded to 2^-9 themselves, take one term.  The row sums
 // add the fp32 values.
 #include <float.h>
 #include <math.h>
@@ -404,7 +404,7 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
   bf16x8 qf[RB][DC];
   int lim[RB];
   float m[RB], l[RB];
-  floatx4 o[RB][DB], sc[4][RB];
+  floatx4 o[RB][DB], ex[4][RB];
   const bool neg = a.scale_log2 < 0.f;
   const float sl2 = fabsf(a.scale_log2);
   const int g = a.Hq / a.Hkv, kg = a.k * g;
@@ -473,7 +473,14 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
     }
   };
   auto lane_max = [&](const floatx4& s, float top) {
-    return fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), top);
+    return fmaxf(fmaxf(fmaxf(fmaxf(top, s[0]), s[1]), s[2]), s[3]);   // two instructions
+  };
+  // (max, sum) of the softmax stand apart from S by exponents S sl2 - m.  Maxima are
+  // taken over them, not over S: the compiler knows a fused product's result for
+  // quiet and needs no instruction to make it so
+  auto exponents = [&](floatx4& s, int rb) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = fmaf(s[i], sl2, -m[rb]);
   };
   // the same over the keys that row block rb may see, s those from key t on: a
   // masked score that exceeds all visible ones by 2^126 would leave them no weight
@@ -494,7 +501,7 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
     const uint32_t dh = PH >= 0 ? 0u : (uint32_t)(x % NBUF) * HALF;
     const uint32_t dn = PH >= 0 ? 0u : (uint32_t)((x + 1) % NBUF) * HALF;
     constexpr int G0 = NEXT ? 0 : NQK;         // the last tile has no scores to form
-    bf16x8 p16[TERMS][2][RB];                  // weights as sums of bf16 terms
+    Pack8 p16[TERMS][2][RB];                   // weights as sums of bf16 terms
     floatx4 sn[4][RB];
     float lm[RB];
     auto weights = [&](int kb) {
@@ -503,16 +510,22 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
         float p[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          p[i] = fast_exp2(fmaf(sc[kb][rb][i], sl2, -m[rb]));
+          p[i] = fast_exp2(ex[kb][rb][i]);
           if constexpr (MASK) {
             if (t0 + kb * 16 + 4 * G4 + i > lim[rb]) p[i] = 0.f;
           }
-          float rest = p[i];
+          if constexpr (TERMS == 1) p16[0][kb >> 1][rb].b[(kb & 1) * 4 + i] = float_to_bf16(p[i]);
+        }
+        if constexpr (TERMS > 1) {             // the upper halves of p and of what they leave, exactly
+          float rest[4] = {p[0], p[1], p[2], p[3]};
 #pragma unroll
           for (int t = 0; t < TERMS; ++t) {
-            const __bf16 x16 = float_to_bf16(rest);
-            p16[t][kb >> 1][rb][(kb & 1) * 4 + i] = x16;
-            rest -= bf16_to_float(x16);        // exact
+#pragma unroll
+            for (int i = 0; i < 4; i += 2)
+              p16[t][kb >> 1][rb].u[(kb & 1) * 2 + i / 2] =
+                  __builtin_amdgcn_perm(__float_as_uint(rest[i + 1]), __float_as_uint(rest[i]), 0x07060302u);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) rest[i] -= __uint_as_float(__float_as_uint(rest[i]) & 0xffff0000u);
           }
         }
         l[rb] += (p[0] + p[1]) + (p[2] + p[3]);
@@ -546,7 +559,7 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
           for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
             for (int t = TERMS - 1; t >= 0; --t)
-              o[rb][4 * pb + d] = mfma_bf16(vv.b, p16[t][hf][rb], o[rb][4 * pb + d]);
+              o[rb][4 * pb + d] = mfma_bf16(vv.b, p16[t][hf][rb].b, o[rb][4 * pb + d]);
           }
         }
         if constexpr (NEXT) {
@@ -554,6 +567,7 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
           for (int kb = q * per; kb < (q + 1) * per; ++kb)
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
+              exponents(sn[kb][rb], rb);
               if constexpr (MASK)
                 lm[rb] = seen_max(sn[kb][rb], t0 + TK + kb * 16 + 4 * G4, rb, kb == 0 ? -FLT_MAX : lm[rb]);
               else
@@ -568,22 +582,26 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
       // lse = m + log2 l
       bool over = false;
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) over = over || fmaf(lm[rb], sl2, -m[rb]) > kHeadroom;
+      for (int rb = 0; rb < RB; ++rb) over = over || lm[rb] > kHeadroom;
       if (__ballot(over) != 0ull) {
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-          const float top = fmaxf(m[rb], wave_max_across_groups(lm[rb]) * sl2);
-          const float f = fast_exp2(m[rb] - top);
+          const float top = m[rb] + fmaxf(wave_max_across_groups(lm[rb]), 0.f);
+          const float up = top - m[rb], f = fast_exp2(-up);
           l[rb] *= f;
 #pragma unroll
           for (int db = 0; db < DB; ++db) o[rb][db] *= f;
+#pragma unroll
+          for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sn[kb][rb][i] -= up;
           m[rb] = top;
         }
       }
 #pragma unroll
       for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) sc[kb][rb] = sn[kb][rb];
+        for (int rb = 0; rb < RB; ++rb) ex[kb][rb] = sn[kb][rb];
     }
   };
 
@@ -620,7 +638,7 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
         reads(gtag, Const<0>{}, Const<0>{}, d0, 0u, Const<0>{});
         lds_wait();
         reads(gtag, Const<0>{}, Const<0>{}, d0, 0u, Const<1>{});
-        scores(gtag, sc);
+        scores(gtag, ex);
       });
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
@@ -628,9 +646,11 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
         lim[rb] = seg.u >= a.G ? seg.L - a.k + r % kg / g : seg.L - 1;
         float top = -FLT_MAX;
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) top = seen_max(sc[kb][rb], t_first + kb * 16 + 4 * G4, rb, top);
+        for (int kb = 0; kb < 4; ++kb) top = seen_max(ex[kb][rb], t_first + kb * 16 + 4 * G4, rb, top);
         top = wave_max_across_groups(top);
         m[rb] = top == -FLT_MAX ? 0.f : top * sl2;      // 0: no key here, l stays 0
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) exponents(ex[kb][rb], rb);
         l[rb] = 0.f;
 #pragma unroll
         for (int db = 0; db < DB; ++db) o[rb][db] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -662,17 +682,19 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
     for (; i < steps - 1; ++i, ++x) step(x, t_first + i * TK, Const<-1>{}, Const<1>{}, Const<1>{});
     step(x, t_first + i * TK, Const<-1>{}, Const<0>{}, Const<1>{});
     ++x;
+    int row = c, ch = 4 * G4;                  // (formed here: no registers for them through the steps)
+    asm volatile("" : "+v"(row), "+v"(ch));
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       const float lsum = wave_sum_across_groups(l[rb]);
-      const int lr = (w * RB + rb) * 16 + c;
+      const int lr = (w * RB + rb) * 16 + row;
       if (seg.rt * ROWS + lr >= seg.rows) continue;
       const size_t prow = part_row<ROWS>(a, seg.u >= a.G, seg.pair, wg) + lr;
       const float inv = lsum != 0.f ? 1.f / lsum : 0.f;   // (a NaN stays one)
 #pragma unroll
       for (int db = 0; db < DB; ++db)
-        *reinterpret_cast<floatx4*>(a.part_o + prow * D + db * 16 + 4 * G4) = o[rb][db] * inv;
-      if (G4 == 0) a.part_lse[prow] = lsum != 0.f ? m[rb] + log2f(lsum) : -INFINITY;
+        *reinterpret_cast<floatx4*>(a.part_o + prow * D + db * 16 + ch) = o[rb][db] * inv;
+      if (ch == 0) a.part_lse[prow] = lsum != 0.f ? m[rb] + log2f(lsum) : -INFINITY;
     }
     if (!more) break;
     busy = load_rows(cc);
