@@ -283,11 +283,10 @@ __device__ __forceinline__ int out_row(const SharedArgs& a, int first, int hk, i
 // ahead and waited for by count.  K and V have rings of four slots: a tile's copy
 // has two steps to land.
 //   64 rows over 65500 keys of 8 heads of 128 (268 MB): 50 us, 5.4 TB/s, HBM.
-//   1024 rows there, bf16 out (275 GFLOP): 265 us, 1040 TFLOP/s, where a matrix
-// product of 8192^3 reaches 1346.  Matrix cores busy 49%, no LDS conflicts, clock
-// 2.05 GHz; without the exponentials (in a copy of the kernel) 11% less time,
-// without P V 12%, without the fragment reads 5%, without the copies 2%: no unit
-// binds alone.
+//   1024 rows there, bf16 out (275 GFLOP): 253 us, 1090 TFLOP/s, where a matrix
+// product of 8192^3 reaches 1346.  Matrix cores busy 50%, no LDS conflicts.  A
+// step's 64 matrix instructions take 1024 cycles of a wave, its 130 vector ones (32
+// of them exponentials) about 900; the two waves of a SIMD overlap them little.
 template <int V>
 struct Const {
   static constexpr int value = V;
