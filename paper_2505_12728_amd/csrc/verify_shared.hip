@@ -1026,10 +1026,12 @@ SharedPlan plan_shared(int B, int k, int Hq, int Hkv, int D, int G, int prefix_c
     p.rows_wg = kRowsF32;
     per_cu = 2;
   } else {
-    // 256 rows halve the copies and LDS reads per row, but a tile of 128 takes
-    // 5/8 of the time of one of 256 (1024 rows, 65500 keys: 340 us in tiles of
-    // 128, 280 in tiles of 256; 384 rows, 16001 keys: 55 and 62), so the places of
-    // the list decide, with groups of average size and every cache at capacity.
+    // 256 rows halve the copies and LDS reads per row: a tile of them takes 2.05 us
+    // where two of 128 take 2.9, but twice the partials cost the call about 7 us.
+    // So the places of the list decide (a third of a tile each, see above), with
+    // groups of average size and every cache at capacity.  In tiles of 128 and of
+    // 256: 256 rows over 16000 keys 41 and 45 us, over 65536 109 and 96; 384 rows
+    // 52 and 54, 512 rows 63 and 60, 768 rows 87 and 74; 1024 over 65500 390 and 293.
     // fp32 outputs take three terms of P, for which 256 rows leave no registers.
     const long long avg = (rows + G - 1) / G;
     auto places = [&](int rows_wg) {
@@ -1040,7 +1042,7 @@ SharedPlan plan_shared(int B, int k, int Hq, int Hkv, int D, int G, int prefix_c
       return Hkv * (of(G * ((avg + rows_wg - 1) / rows_wg), avg, prefix_cap) +
                     of(B * (long long)((kg + rows_wg - 1) / rows_wg), kg, cap));
     };
-    p.rows_wg = out_bf16 && places(256) * 8 <= places(128) * 5 ? 256 : 128;
+    p.rows_wg = out_bf16 && 41 * places(256) + 420LL * cus <= 29 * places(128) ? 256 : 128;   // (us * 60)
   }
   const int tk = dtype == 0 ? kTileF32 : kTile;
   p.rows_own = std::min((kg + 15) / 16 * 16, p.rows_wg);

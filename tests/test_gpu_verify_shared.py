@@ -70,6 +70,22 @@ def call(d, **kw):
     return sd.sd_verify_shared(**args)
 
 
+def roomy(d, keys=1 << 18):
+    """The prefixes in caches of `keys` keys, what lies behind them not a number:
+    with many rows the capacity decides on tiles of 256 rows."""
+    import torch
+    if d["prefix_table"] is not None:
+        t = torch.full((len(d["prefix_len"]), keys // 16), -1, dtype=torch.int32, device="cuda")
+        t[:, :d["prefix_table"].shape[1]] = torch.as_tensor(d["prefix_table"]).cuda()
+        return dict(prefix_table=t)
+    big = {}
+    for n in ("k_prefix", "v_prefix"):
+        G, L, Hkv, D = d[n].shape
+        big[n] = torch.full((G, keys, Hkv, D), math.nan, dtype=d[n].dtype, device="cuda")
+        big[n][:, :L] = d[n].cuda()
+    return big
+
+
 def reference(d, scale):
     f = lambda t: None if t is None else t.double().numpy()               # noqa: E731
     kp = d["k_prefix"] if d["k_prefix"] is not None else d["k_cache"]
@@ -134,6 +150,23 @@ def test_shared(case, kind):
     check(d, out, lse, reference(d, 1 / math.sqrt(D)), kind)
 
 
+@pytest.mark.parametrize("case", [
+    ([20] * 32, [333], [32], 8, 1, 1, 128, False, 0, 0),
+    ([64, 5] * 20, [500, 300], [31, 9], 4, 28, 4, 128, True, 0, 0),
+    ([33] * 16, [1025], [16], 16, 2, 2, 128, True, 0, 0),
+    ([40] * 37, [700], [37], 7, 8, 4, 64, False, 0, 0),
+    ([0, 3, 70, 9] * 12, [65, 0, 900], [30, 0, 18], 5, 16, 1, 128, False, 0, 0),
+    ([100, 16, 8], [90], [3], 16, 16, 1, 64, True, 0, 0),
+], ids=lambda c: f"B{len(c[0])}G{len(c[1])}k{c[3]}h{c[4]}x{c[5]}d{c[6]}p{c[7]:d}")
+@pytest.mark.parametrize("kind", ["hilo", "bf16"])
+def test_shared_roomy_caches(case, kind):
+    import torch
+    lens, plens, sizes, k, Hq, Hkv, D, paged, lead, left = case
+    d = inputs(lens, plens, sizes, k, Hq, Hkv, D, "bf16", paged, len(lens), lead, left)
+    out, lse = call(d, out_dtype=torch.bfloat16 if kind == "bf16" else torch.float32, **roomy(d))
+    check(d, out, lse, reference(d, 1 / math.sqrt(D)), kind)
+
+
 @pytest.mark.parametrize("units", [-1.0, 0.0, 6.0])
 @pytest.mark.parametrize("kind", ["hilo", "bf16"])
 def test_shared_scales(units, kind):
@@ -154,10 +187,13 @@ def test_shared_rising_scores(rows):
     d["q"].fill_(0.25)
     ramp = torch.linspace(0, 12, 400)[:, None, None]
     d["k_prefix"][0, :400] = (ramp + 0.01 * d["k_prefix"][0, :400].float()).to(torch.bfloat16)
-    out, lse = call(d, scale=1.0)
     # scores reach 16 * 12 = 192 from 64 products of one sign: their float32
     # sum is off by at most 64 * 2^-24 * 192, within the bound for n = 8
-    check(d, out, lse, reference(d, 1.0), "hilo", 8.0)
+    ref = reference(d, 1.0)
+    out, lse = call(d, scale=1.0)
+    check(d, out, lse, ref, "hilo", 8.0)
+    out, lse = call(d, scale=1.0, out_dtype=torch.bfloat16, **roomy(d))
+    check(d, out, lse, ref, "bf16", 8.0)
 
 
 @pytest.mark.parametrize("k,lens", [(4, [4, 5, 70]), (16, [16, 65, 79, 130]), (2, [1, 2, 66])])
@@ -177,7 +213,7 @@ def test_shared_masked_keys_weigh_nothing(k, lens, rows, prefix):
         d["k_cache"][b, n - 1] = 8.0
     ref = reference(d, 1.0)
     for kind in ("hilo", "bf16"):
-        out, lse = call(d, scale=1.0, out_dtype=torch.bfloat16 if kind == "bf16" else torch.float32)
+        out, lse = call(d, scale=1.0, out_dtype=torch.bfloat16 if kind == "bf16" else torch.float32, **roomy(d))
         # 512 log2(e) is held to about 2^-14 in the last row's lse
         check(d, out, lse, ref, kind)
 
