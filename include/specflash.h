@@ -656,7 +656,7 @@ int sd_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_strid
  *               sd_verify_attention
  * SD_BF16 with out_dtype SD_F32 feeds the probabilities to the second product
  * as sums of three bf16 (all of their float32 bits); with out_dtype SD_BF16 as
- * one bf16 each (2^-9, the rounding of out itself), half the matrix work.
+ * sums of two (16 bits, below the rounding of out itself).
  * SD_F32 runs in float64 and gives SD_F32.
  * Requirements: those of sd_verify_attention for k, Hq, Hkv, D, scale and
  * alignment; 1 <= G <= B <= 2^16; Hq <= 2^16; B k Hq < 2^31; fewer than 2^27

@@ -23,11 +23,13 @@
 // Kernel 2 (merge).  Finds the partials of a row's prefix pair and of its own pair
 //   from the same arithmetic and combines them.
 //
-// P goes into the second product as bf16.  fp32 outputs take it as the sum of
-// three bf16 terms (all 24 bits of p, eight each, three products): two would leave
-// 2e-6 of the output, where fp32 products leave 4e-7, and cost 14% less where the
-// matrix cores bound (16 blocks of 6 x 4 rows, 16001 keys: 61 us in two terms, 70
-// in three).  bf16 outputs, rounded to 2^-9 themselves, take one term.  The row sums
+// P goes into the second product as a sum of bf16 terms.  fp32 outputs take three
+// (all 24 bits of p, eight each, three products): two would leave 2e-6 of the
+// output, where fp32 products leave 4e-7, and cost 14% less where the matrix cores
+// bound (16 blocks of 6 x 4 rows, 16001 keys: 61 us in two terms, 70 in three).
+// bf16 outputs take two (16 bits): the output's own rounding is then all that is
+// lost, 1.7e-3 of rms, where a single term left 2.3e-3 and 2^-9 of |V| in outputs
+// that cancel, and took 278 us for 369 (1024 rows over 65500 keys).  The row sums
 // add the fp32 values.
 #include <float.h>
 #include <math.h>
@@ -283,10 +285,10 @@ __device__ __forceinline__ int out_row(const SharedArgs& a, int first, int hk, i
 // ahead and waited for by count.  K and V have rings of four slots: a tile's copy
 // has two steps to land.
 //   64 rows over 65500 keys of 8 heads of 128 (268 MB): 50 us, 5.4 TB/s, HBM.
-//   1024 rows there, bf16 out (275 GFLOP): 253 us, 1090 TFLOP/s, where a matrix
-// product of 8192^3 reaches 1346.  Matrix cores busy 50%, no LDS conflicts.  A
-// step's 64 matrix instructions take 1024 cycles of a wave, its 130 vector ones (32
-// of them exponentials) about 900; the two waves of a SIMD overlap them little.
+//   1024 rows there, bf16 out (275 GFLOP in the formula, 413 in two terms):
+// the call with its merge 369 us, 1120 TFLOP/s of products, where one of 8192^3
+// reaches 1346.  No LDS conflicts.  A step's 96 matrix instructions take 1536
+// cycles of a wave.
 template <int V>
 struct Const {
   static constexpr int value = V;
@@ -513,19 +515,23 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
           if constexpr (MASK) {
             if (t0 + kb * 16 + 4 * G4 + i > lim[rb]) p[i] = 0.f;
           }
-          if constexpr (TERMS == 1) p16[0][kb >> 1][rb].b[(kb & 1) * 4 + i] = float_to_bf16(p[i]);
         }
-        if constexpr (TERMS > 1) {             // the upper halves of p and of what they leave, exactly
-          float rest[4] = {p[0], p[1], p[2], p[3]};
+        // the upper halves of p and of what they leave, exactly; the last of two
+        // terms rounded
+        float rest[4] = {p[0], p[1], p[2], p[3]};
 #pragma unroll
-          for (int t = 0; t < TERMS; ++t) {
+        for (int t = 0; t < TERMS; ++t) {
+          if (TERMS == 2 && t == 1) {
 #pragma unroll
-            for (int i = 0; i < 4; i += 2)
-              p16[t][kb >> 1][rb].u[(kb & 1) * 2 + i / 2] =
-                  __builtin_amdgcn_perm(__float_as_uint(rest[i + 1]), __float_as_uint(rest[i]), 0x07060302u);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) rest[i] -= __uint_as_float(__float_as_uint(rest[i]) & 0xffff0000u);
+            for (int i = 0; i < 4; ++i) p16[t][kb >> 1][rb].b[(kb & 1) * 4 + i] = float_to_bf16(rest[i]);
+            continue;
           }
+#pragma unroll
+          for (int i = 0; i < 4; i += 2)
+            p16[t][kb >> 1][rb].u[(kb & 1) * 2 + i / 2] =
+                __builtin_amdgcn_perm(__float_as_uint(rest[i + 1]), __float_as_uint(rest[i]), 0x07060302u);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) rest[i] -= __uint_as_float(__float_as_uint(rest[i]) & 0xffff0000u);
         }
         l[rb] += (p[0] + p[1]) + (p[2] + p[3]);
       }
@@ -1026,12 +1032,12 @@ SharedPlan plan_shared(int B, int k, int Hq, int Hkv, int D, int G, int prefix_c
     p.rows_wg = kRowsF32;
     per_cu = 2;
   } else {
-    // 256 rows halve the copies and LDS reads per row: a tile of them takes 2.05 us
-    // where two of 128 take 2.9, but twice the partials cost the call about 7 us.
+    // 256 rows halve the copies and LDS reads per row: a tile of them takes 2.6 us
+    // where two of 128 take 3.2, but twice the partials cost the call about 7.5 us.
     // So the places of the list decide (a third of a tile each, see above), with
     // groups of average size and every cache at capacity.  In tiles of 128 and of
-    // 256: 256 rows over 16000 keys 41 and 45 us, over 65536 109 and 96; 384 rows
-    // 52 and 54, 512 rows 63 and 60, 768 rows 87 and 74; 1024 over 65500 390 and 293.
+    // 256: 256 rows over 16000 keys 47 and 50 us, over 65536 125 and 113; 384 rows
+    // 59 and 63, 512 rows 70 and 69, 768 rows 92 and 89; 1024 over 65500 456 and 383.
     // fp32 outputs take three terms of P, for which 256 rows leave no registers.
     const long long avg = (rows + G - 1) / G;
     auto places = [&](int rows_wg) {
@@ -1042,7 +1048,7 @@ SharedPlan plan_shared(int B, int k, int Hq, int Hkv, int D, int G, int prefix_c
       return Hkv * (of(G * ((avg + rows_wg - 1) / rows_wg), avg, prefix_cap) +
                     of(B * (long long)((kg + rows_wg - 1) / rows_wg), kg, cap));
     };
-    p.rows_wg = out_bf16 && 41 * places(256) + 420LL * cus <= 29 * places(128) ? 256 : 128;   // (us * 60)
+    p.rows_wg = out_bf16 && 52 * places(256) + 450LL * cus <= 32 * places(128) ? 256 : 128;   // (us * 60)
   }
   const int tk = dtype == 0 ? kTileF32 : kTile;
   p.rows_own = std::min((kg + 15) / 16 * 16, p.rows_wg);
@@ -1068,11 +1074,11 @@ hipError_t launch_shared(const SharedArgs& a, const SharedPlan& p, int dtype, hi
     return e != hipSuccess ? e : launch_merge<kRowsF32, kTileF32>(a, p, st);
   }
   if (p.rows_wg == 256) {
-    e = a.D == 128 ? launch_bf16<128, 2, 1>(a, p, st) : launch_bf16<64, 2, 1>(a, p, st);
+    e = a.D == 128 ? launch_bf16<128, 2, 2>(a, p, st) : launch_bf16<64, 2, 2>(a, p, st);
     return e != hipSuccess ? e : launch_merge<256, kTile>(a, p, st);
   }
   if (a.out_bf16)
-    e = a.D == 128 ? launch_bf16<128, 1, 1>(a, p, st) : launch_bf16<64, 1, 1>(a, p, st);
+    e = a.D == 128 ? launch_bf16<128, 1, 2>(a, p, st) : launch_bf16<64, 1, 2>(a, p, st);
   else
     e = a.D == 128 ? launch_bf16<128, 1, 3>(a, p, st) : launch_bf16<64, 1, 3>(a, p, st);
   return e != hipSuccess ? e : launch_merge<128, kTile>(a, p, st);

@@ -1,0 +1,40 @@
+"""sd_verify_shared where its arithmetic can lose bits or rows: bf16 outputs that
+cancel, maxima far above the keys before them, scores of -inf, log-sum-exps of
+thousands joined from many partials, infinite values, merge waves of several rows.
+
+Lists are long enough that a work-group's segment spans several 64-key tiles
+(20000 keys of 8 pairs or more are at least nine tiles for each of 256 of them)."""
+
+import math
+
+import numpy as np
+import pytest
+
+from tests.test_gpu_verify_shared import call, check, inputs, reference, roomy
+
+pytestmark = pytest.mark.gpu
+
+
+def out_type(kind):
+    import torch
+    return torch.bfloat16 if kind == "bf16" else torch.float32
+
+
+# ------------------------------------------------ bf16 outputs that cancel
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("wide", [False, True])
+def test_shared_bf16_outputs_are_off_by_their_own_rounding(D, wide):
+    # few keys of values that cancel: out is far below A, the mean of |V|, and
+    # its own rounding (half a step, 2^-8 of it at most) far below what weights
+    # of eight bits would leave, 2^-9 A.  The rest as for fp32 outputs: 2^-12 A,
+    # of which weights of 16 bits take 2^-16
+    d = inputs([4, 5, 6, 7, 9] * 4, [3], [20], 4, 16, 1, D, seed=31)
+    for n in ("v_cache", "v_prefix"):
+        sign = d[n].float().sign()
+        d[n] = (sign * (1 + d[n].float().abs() / 64)).to(d[n].dtype)
+    ro, rl, A = reference(d, 1 / math.sqrt(D))
+    out, lse = call(d, out_dtype=out_type("bf16"), **(roomy(d) if wide else {}))
+    err = np.abs(out.double().cpu().numpy() - ro) - 2.0 ** -8 * np.abs(ro) - 2.0 ** -12 * A
+    assert np.all(err <= 0), err.max()
+    assert np.all(np.abs(lse.cpu().numpy() - rl) <= 2.0 ** -12)
