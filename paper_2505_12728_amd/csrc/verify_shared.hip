@@ -584,23 +584,39 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
     });
     if constexpr (NEXT) {
       // m, raised only where an exponent passes 2^24, cancels in o = O / l and
-      // lse = m + log2 l
+      // lse = m + log2 l.  The exponents, rounded after the difference, have lost
+      // what an m far below the scores dwarfs: the scores are formed again from the
+      // tile's fragments, which lie in LDS until step x + 2, and the exponents from
+      // the new maximum
       bool over = false;
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) over = over || lm[rb] > kHeadroom;
       if (__ballot(over) != 0ull) {
+        const uint32_t d1 = (uint32_t)((x + 1) % NBUF) * HALF;
+        unrolled<0, NQK>([&](auto gtag) {
+          reads(gtag, Const<0>{}, Const<0>{}, d1, 0u, Const<0>{});
+          lds_wait();
+          reads(gtag, Const<0>{}, Const<0>{}, d1, 0u, Const<1>{});
+          scores(gtag, sn);
+        });
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-          const float top = m[rb] + fmaxf(wave_max_across_groups(lm[rb]), 0.f);
-          const float up = top - m[rb], f = fast_exp2(-up);
+          float top = -FLT_MAX;
+#pragma unroll
+          for (int kb = 0; kb < 4; ++kb) {
+            if constexpr (MASK)
+              top = seen_max(sn[kb][rb], t0 + TK + kb * 16 + 4 * G4, rb, top);
+            else
+              top = lane_max(sn[kb][rb], top);
+          }
+          top = fmaxf(wave_max_across_groups(top) * sl2, m[rb]);
+          const float f = fast_exp2(m[rb] - top);
           l[rb] *= f;
 #pragma unroll
           for (int db = 0; db < DB; ++db) o[rb][db] *= f;
-#pragma unroll
-          for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sn[kb][rb][i] -= up;
           m[rb] = top;
+#pragma unroll
+          for (int kb = 0; kb < 4; ++kb) exponents(sn[kb][rb], rb);
         }
       }
 #pragma unroll

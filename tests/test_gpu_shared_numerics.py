@@ -38,3 +38,33 @@ def test_shared_bf16_outputs_are_off_by_their_own_rounding(D, wide):
     err = np.abs(out.double().cpu().numpy() - ro) - 2.0 ** -8 * np.abs(ro) - 2.0 ** -12 * A
     assert np.all(err <= 0), err.max()
     assert np.all(np.abs(lse.cpu().numpy() - rl) <= 2.0 ** -12)
+
+
+# --------------------------------------------- maxima far above those before
+
+def long_groups(rows, seed, keys=20000, Hkv=4, D=64, dtype="bf16"):
+    """One group of `rows` rows a KV head over one long prefix; q[.., 0] is 1."""
+    d = inputs([8] * (rows // 8), [keys], [rows // 8], 8, Hkv, Hkv, D, dtype, seed=seed)
+    d["q"][..., 0] = 1.0
+    for n in ("k_cache", "k_prefix"):
+        d[n][..., 0] = 0.0
+    return d
+
+
+def every_other_tile(d, channel, value):
+    n = int(d["prefix_len"][0])
+    low = np.nonzero(np.arange(n) // 64 % 2 == 0)[0]
+    d["k_prefix"][0, low, :, channel] = value
+
+
+@pytest.mark.parametrize("low", [50.0, 5e4, 1e6, 1e8])
+@pytest.mark.parametrize("rows", [64, 256])
+def test_shared_tiles_far_below_the_maximum(low, rows):
+    # every other tile of 64 keys lies lower by `low`: segments that begin in
+    # one raise their maximum by that much, and the tiles above it keep their bits
+    d = long_groups(rows, seed=32)
+    every_other_tile(d, 0, -8 * low)
+    ref = reference(d, 1 / 8)
+    for kind in ("hilo", "bf16"):
+        out, lse = call(d, out_dtype=out_type(kind), **(roomy(d) if kind == "bf16" else {}))
+        check(d, out, lse, ref, kind)
