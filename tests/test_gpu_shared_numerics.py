@@ -68,3 +68,37 @@ def test_shared_tiles_far_below_the_maximum(low, rows):
     for kind in ("hilo", "bf16"):
         out, lse = call(d, out_dtype=out_type(kind), **(roomy(d) if kind == "bf16" else {}))
         check(d, out, lse, ref, kind)
+
+
+# ------------------------------------------------------- scores of -inf
+
+@pytest.mark.parametrize("how", ["overflow", "key"])
+@pytest.mark.parametrize("rows", [64, 256])
+@pytest.mark.parametrize("level", [-300.0, 300.0])
+def test_shared_tiles_of_minus_infinity(how, rows, level):
+    # every other tile's scores are -inf (a product past fp32's range, or a key of
+    # -inf): weight 0, and the tiles behind one are as they are alone, wherever
+    # their own scores lie
+    d = long_groups(rows, seed=33)
+    d["q"][..., 0] = 1e20 if how == "overflow" else 1.0
+    d["q"][..., 1] = 1.0
+    for n in ("k_cache", "k_prefix"):
+        d[n][..., 1] = 8 * level
+    every_other_tile(d, 0, -1e20 if how == "overflow" else -math.inf)
+    ref = reference(d, 1 / 8)
+    # the products' sum passes 300 sqrt(D): bound of the scores as for a scale of
+    # 300 / 8 units
+    for kind in ("hilo", "bf16"):
+        out, lse = call(d, out_dtype=out_type(kind), **(roomy(d) if kind == "bf16" else {}))
+        check(d, out, lse, ref, kind, 300 / 8)
+
+
+@pytest.mark.parametrize("kind", ["hilo", "bf16", "f32"])
+def test_shared_only_minus_infinity_is_no_key(kind):
+    # rows all of whose scores are -inf see nothing: out 0 and lse -inf
+    d = inputs([40, 300], [200], [2], 4, 4, 2, 64, "f32" if kind == "f32" else "bf16", seed=34)
+    d["q"][..., 0] = 1.0
+    for n in ("k_cache", "k_prefix"):
+        d[n][..., 0] = -math.inf
+    out, lse = call(d, out_dtype=out_type(kind))
+    assert not out.any() and bool((lse == -math.inf).all())
