@@ -270,6 +270,7 @@ struct SharedPlan {
   int wgs;              // grid of the stream kernel
   long long own_base;   // first such row among the partials
   size_t part_rows;
+  size_t ml_offset;     // bytes of the workspace before the partials' maxima and sums
   size_t workspace_bytes;
   bool ok;              // false: the shape exceeds the kernels' index range
 };
@@ -292,8 +293,8 @@ struct SharedArgs {
   bool out_bf16;
   int B, k, Hq, Hkv, D, G;
   float scale, scale_log2;
-  float* part_o;              // [part_rows, D] partial outputs (normalised)
-  float* part_lse;            // [part_rows] partial log-sum-exp (log2 units)
+  void* part_o;               // [part_rows, D] partial outputs (normalised): float32, or float64 for fp32 inputs
+  void* part_ml;              // [part_rows, 2] their maxima and sums, same type
   int rows_own;
   long long own_base;
 };

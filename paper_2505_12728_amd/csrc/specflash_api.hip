@@ -925,8 +925,8 @@ int sd_verify_shared(const void* q, const void* k_cache, const void* v_cache, co
   a.G = G;
   a.scale = scale;
   a.scale_log2 = scale * 1.4426950408889634f;
-  a.part_o = static_cast<float*>(workspace);
-  a.part_lse = a.part_o + plan.part_rows * D;
+  a.part_o = workspace;
+  a.part_ml = static_cast<unsigned char*>(workspace) + plan.ml_offset;
   a.rows_own = plan.rows_own;
   a.own_base = plan.own_base;
   return status_from(sd::launch_shared(a, plan, dtype, static_cast<hipStream_t>(stream)));

@@ -19,9 +19,11 @@
 //   tile, and lengths and groups are read on the device alone.  A tile's keys and
 //   values pass through LDS once for all ROWS rows:  S^T = K Q^T, online softmax
 //   in fp32 (base 2), O^T += V^T P^T.  Where its range leaves a pair, a work-group
-//   writes the segment's normalised partial (o, lse).
+//   writes the segment's partial: its normalised output, its maximum and its sum.
 // Kernel 2 (merge).  Finds the partials of a row's prefix pair and of its own pair
-//   from the same arithmetic and combines them.
+//   from the same arithmetic and combines them.  Maximum and sum come apart: a
+//   log-sum-exp in one float would be off by half a step of its own size, 5e-6 of
+//   a partial's weight at scores of 100, 1e-3 at 30000.
 //
 // P goes into the second product as a sum of bf16 terms.  fp32 outputs take three
 // (all 24 bits of p, eight each, three products): two would leave 2e-6 of the
@@ -35,6 +37,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "device_common.hpp"
 #include "launch.hpp"
@@ -269,6 +272,17 @@ template <int ROWS>
 __device__ __forceinline__ size_t part_row(const SharedArgs& a, bool own, int pair, int w) {
   return own ? (size_t)a.own_base + (size_t)(pair + w) * a.rows_own : (size_t)(pair + w) * ROWS;
 }
+
+// Partials and their merge: float32, maxima in log2 units; float64 for fp32
+// inputs, maxima of the scores themselves.
+template <typename T, int N>
+using Vec = T __attribute__((ext_vector_type(N)));
+template <int ROWS>
+using PartT = std::conditional_t<ROWS == kRowsF32, double, float>;
+__device__ __forceinline__ float weight_of(float x) { return exp2f(x); }
+__device__ __forceinline__ double weight_of(double x) { return exp(x); }
+__device__ __forceinline__ float lse_of(float m, float l) { return (m + log2f(l)) * kLn2; }
+__device__ __forceinline__ float lse_of(double m, double l) { return (float)(m + log(l)); }
 
 // output row (flat over [B, k, Hq]) of row r of a unit that starts at sequence `first`
 __device__ __forceinline__ int out_row(const SharedArgs& a, int first, int hk, int r) {
@@ -584,7 +598,7 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
     });
     if constexpr (NEXT) {
       // m, raised only where an exponent passes 2^24, cancels in o = O / l and
-      // lse = m + log2 l.  The exponents, rounded after the difference, have lost
+      // lse = m + log2 l (in log2 units).  The exponents, rounded after the difference, have lost
       // what an m far below the scores dwarfs: the scores are formed again from the
       // tile's fragments, which lie in LDS until step x + 2, and the exponents from
       // the new maximum
@@ -716,8 +730,8 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
       const float inv = lsum != 0.f ? 1.f / lsum : 0.f;   // (a NaN stays one)
 #pragma unroll
       for (int db = 0; db < DB; ++db)
-        *reinterpret_cast<floatx4*>(a.part_o + prow * D + db * 16 + ch) = o[rb][db] * inv;
-      if (ch == 0) a.part_lse[prow] = lsum != 0.f ? m[rb] + log2f(lsum) : -INFINITY;
+        *reinterpret_cast<floatx4*>(static_cast<float*>(a.part_o) + prow * D + db * 16 + ch) = o[rb][db] * inv;
+      if (ch == 0) static_cast<Vec<float, 2>*>(a.part_ml)[prow] = {lsum != 0.f ? m[rb] : -INFINITY, lsum};
     }
     if (!more) break;
     busy = load_rows(cc);
@@ -726,7 +740,7 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
 }
 
 // ------------------------------------------------------------- fp32 stream
-// fp32 inputs: scores, softmax and P V in float64, as everywhere for fp32.
+// fp32 inputs: scores, softmax, P V and partials in float64.
 // The same list with 16 rows per work-group and 32-key tiles.  The segment's
 // queries and a tile's keys and values lie in LDS (rows padded by one float);
 // row r belongs to the 16 lanes r * 16 ..: each forms two of its scores, its
@@ -840,8 +854,10 @@ __global__ __launch_bounds__(256) void shared_stream_f32(SharedArgs a, int G) {
     if ((fresh || end) && row < cu.rows) {
       const size_t at = part_row<R>(a, own, cu.pair, wg) + r;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) a.part_o[at * D + lane16 + 16 * e] = l != 0.0 ? (float)(o[e] / l) : 0.f;
-      if (lane16 == 0) a.part_lse[at] = l != 0.0 ? (float)((m + log(l)) * 1.4426950408889634) : -INFINITY;
+      for (int e = 0; e < PER; ++e)
+        static_cast<double*>(a.part_o)[at * D + lane16 + 16 * e] = l != 0.0 ? o[e] / l : 0.0;
+      // (a sum that is not a number may stand beside a maximum of none: never a partial without keys)
+      if (lane16 == 0) static_cast<Vec<double, 2>*>(a.part_ml)[at] = {l == l ? m : l, l};
     }
     if (end) break;
     advance<R, TK>(a, cu);
@@ -854,15 +870,16 @@ __global__ __launch_bounds__(256) void shared_stream_f32(SharedArgs a, int G) {
 // wrote one partial (with few places, the owners of its tiles did).  A row's
 // candidates are the partials of its prefix pair, then of its own pair.  A wave
 // holds the row's channels (D / 64 per lane) and takes 8 candidates at a time:
-// their lse are the same on every lane, so that their weights 2^(lse - max) need
-// no exchange between lanes.  Few rows have many candidates each and take the
+// their (max, sum) are the same on every lane, so that their weights need no
+// exchange between lanes.  Few rows have many candidates each and take the
 // four waves of a work-group (SPLIT), joined in LDS; otherwise a wave takes
 // `per` rows of one sequence, so that the scan over the units is made once for
 // them.  Bound by latency while rows are few, by the partials' bytes beyond.
 template <int ROWS, int TK, int D, bool SPLIT>
 __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G, int per, int wgs_seq) {
   constexpr int CH = D / 64, ROUND = 8;
-  __shared__ float part[4][2 + D];             // SPLIT: each wave's max, sum and channels
+  using F = PartT<ROWS>;
+  __shared__ F part[4][2 + D];                // SPLIT: each wave's max, sum and channels
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int b = blockIdx.x / wgs_seq;
   const int row0 = ((blockIdx.x - b * wgs_seq) * (SPLIT ? 1 : 4) + (SPLIT ? 0 : w)) * per;   // of the k Hq rows of b
@@ -918,47 +935,45 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G, int per
       nc[kind] = sparse ? nt[kind] : owner(U[kind] + (nt[kind] - 1) * wt[kind]) - wf[kind] + 1;
     }
     const int ncand = nc[0] + nc[1];
-    float mx = -INFINITY, wsum = 0.f, acc[CH];
+    F mx = -INFINITY, wsum = 0, acc[CH];
 #pragma unroll
-    for (int e = 0; e < CH; ++e) acc[e] = 0.f;
+    for (int e = 0; e < CH; ++e) acc[e] = 0;
     for (int c0 = SPLIT ? w * ROUND : 0; c0 < ncand; c0 += SPLIT ? 4 * ROUND : ROUND) {
-      float ls[ROUND], po[ROUND][CH];
+      F ms[ROUND], ls[ROUND];                  // maximum and sum
+      Vec<F, CH> po[ROUND];
 #pragma unroll
       for (int i = 0; i < ROUND; ++i) {
         const int cand = min(c0 + i, ncand - 1);
         const int kind = cand >= nc[0], k = cand - (kind ? nc[0] : 0);
-        const int wv = sparse ? owner(U[kind] + k * wt[kind]) : wf[kind] + k;
-        const size_t prow = (size_t)(first[kind] + (long long)wv * (kind ? a.rows_own : ROWS));
-        ls[i] = a.part_lse[prow];
-        if (sparse && k > 0 && owner(U[kind] + (k - 1) * wt[kind]) == wv) ls[i] = -INFINITY;
-        const float* src = a.part_o + prow * D + lane * CH;
-        if constexpr (CH == 2) {
-          const float2 v = *reinterpret_cast<const float2*>(src);
-          po[i][0] = v.x;
-          po[i][1] = v.y;
-        } else {
-          po[i][0] = src[0];
+        int wv = wf[kind] + k, prev = -1;      // owners of this tile and of the one before
+        if (sparse) {
+          wv = owner(U[kind] + k * wt[kind]);
+          if (k > 0) prev = owner(U[kind] + (k - 1) * wt[kind]);
         }
+        const size_t prow = (size_t)(first[kind] + (long long)wv * (kind ? a.rows_own : ROWS));
+        const Vec<F, 2> ml = static_cast<const Vec<F, 2>*>(a.part_ml)[prow];
+        po[i] = *reinterpret_cast<const Vec<F, CH>*>(static_cast<const F*>(a.part_o) + prow * D + lane * CH);
+        ms[i] = c0 + i < ncand && wv != prev ? ml[0] : -INFINITY;
+        ls[i] = ml[1];
       }
-      float nm = mx;
+      F nm = mx;
       bool none = mx == -INFINITY;
 #pragma unroll
       for (int i = 0; i < ROUND; ++i) {
-        if (c0 + i >= ncand) ls[i] = -INFINITY;
-        nm = fmaxf(nm, ls[i]);
-        none = none && ls[i] == -INFINITY;
+        nm = fmax(nm, ms[i]);
+        none = none && ms[i] == -INFINITY;
       }
       if (none) continue;                      // no key in any partial so far
-      const float keep = exp2f(mx - nm);       // (0 from -inf)
+      const F keep = weight_of(mx - nm);       // (0 from -inf)
       wsum *= keep;
 #pragma unroll
       for (int e = 0; e < CH; ++e) acc[e] *= keep;
 #pragma unroll
       for (int i = 0; i < ROUND; ++i) {
-        const float wl = exp2f(ls[i] - nm);
+        const F wl = weight_of(ms[i] - nm) * ls[i];
         wsum += wl;
 #pragma unroll
-        for (int e = 0; e < CH; ++e) acc[e] = fmaf(wl, po[i][e], acc[e]);
+        for (int e = 0; e < CH; ++e) acc[e] = fma(wl, po[i][e], acc[e]);
       }
       mx = nm;
     }
@@ -970,44 +985,35 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G, int per
       for (int e = 0; e < CH; ++e) part[w][2 + lane * CH + e] = acc[e];
       __syncthreads();
       if (w != 0) continue;
-      float nm = mx;
+      F nm = mx;
 #pragma unroll
-      for (int v = 1; v < 4; ++v) nm = fmaxf(nm, part[v][0]);
-      wsum = 0.f;
+      for (int v = 1; v < 4; ++v) nm = fmax(nm, part[v][0]);
+      wsum = 0;
 #pragma unroll
-      for (int e = 0; e < CH; ++e) acc[e] = 0.f;
+      for (int e = 0; e < CH; ++e) acc[e] = 0;
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        const float f = part[v][0] == nm ? 1.f : exp2f(part[v][0] - nm);   // (-inf too)
-        wsum = fmaf(f, part[v][1], wsum);
+        const F f = part[v][0] == nm ? 1 : weight_of(part[v][0] - nm);   // (-inf too)
+        wsum = fma(f, part[v][1], wsum);
 #pragma unroll
-        for (int e = 0; e < CH; ++e) acc[e] = fmaf(f, part[v][2 + lane * CH + e], acc[e]);
+        for (int e = 0; e < CH; ++e) acc[e] = fma(f, part[v][2 + lane * CH + e], acc[e]);
       }
       mx = nm;
     }
     const size_t orow = (size_t)b * rows + row;
-    const float inv = wsum != 0.f ? 1.f / wsum : 0.f;
-    if (a.out_bf16) {
-      __bf16* dst = static_cast<__bf16*>(a.out) + orow * D + lane * CH;
-      if constexpr (CH == 2) {
-        union {
-          __bf16 b[2];
-          uint32_t u;
-        } v;
-        v.b[0] = float_to_bf16(acc[0] * inv);
-        v.b[1] = float_to_bf16(acc[1] * inv);
-        *reinterpret_cast<uint32_t*>(dst) = v.u;
-      } else {
-        dst[0] = float_to_bf16(acc[0] * inv);
-      }
+    const F inv = wsum != 0 ? 1 / wsum : 0;
+    if (ROWS != kRowsF32 && a.out_bf16) {
+      Vec<__bf16, CH> v;
+#pragma unroll
+      for (int e = 0; e < CH; ++e) v[e] = float_to_bf16((float)(acc[e] * inv));
+      *reinterpret_cast<Vec<__bf16, CH>*>(static_cast<__bf16*>(a.out) + orow * D + lane * CH) = v;
     } else {
-      float* dst = static_cast<float*>(a.out) + orow * D + lane * CH;
-      if constexpr (CH == 2)
-        *reinterpret_cast<float2*>(dst) = make_float2(acc[0] * inv, acc[1] * inv);
-      else
-        dst[0] = acc[0] * inv;
+      Vec<float, CH> v;
+#pragma unroll
+      for (int e = 0; e < CH; ++e) v[e] = (float)(acc[e] * inv);
+      *reinterpret_cast<Vec<float, CH>*>(static_cast<float*>(a.out) + orow * D + lane * CH) = v;
     }
-    if (a.lse != nullptr && lane == 0) a.lse[orow] = wsum != 0.f ? (mx + log2f(wsum)) * kLn2 : -INFINITY;
+    if (a.lse != nullptr && lane == 0) a.lse[orow] = wsum != 0 ? lse_of(mx, wsum) : -INFINITY;
   }
 }
 
@@ -1077,7 +1083,9 @@ SharedPlan plan_shared(int B, int k, int Hq, int Hkv, int D, int G, int prefix_c
   p.wgs = (int)std::max(1LL, std::min((long long)cus * per_cu, tiles));
   p.own_base = (prefix_pairs + p.wgs) * p.rows_wg;
   p.part_rows = (size_t)p.own_base + (size_t)(own_pairs + p.wgs) * p.rows_own;
-  p.workspace_bytes = p.part_rows * ((size_t)D + 1) * sizeof(float);
+  const size_t es = dtype == 0 ? sizeof(PartT<kRowsF32>) : sizeof(float);
+  p.ml_offset = p.part_rows * D * es;
+  p.workspace_bytes = p.ml_offset + p.part_rows * 2 * es;
   return p;
 }
 

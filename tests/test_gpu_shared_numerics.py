@@ -102,3 +102,63 @@ def test_shared_only_minus_infinity_is_no_key(kind):
         d[n][..., 0] = -math.inf
     out, lse = call(d, out_dtype=out_type(kind))
     assert not out.any() and bool((lse == -math.inf).all())
+
+
+# ------------------------------------------ large log-sum-exps in many partials
+
+def high_scores(rows, level, dtype, seed, keys=20000, Hkv=4):
+    """Scores of `level` plus multiples of 2^-6 that float32 sums exactly; values
+    of 1 in the first half of the prefix and of -1 behind it."""
+    import torch
+    d = inputs([8] * (rows // 8), [keys], [rows // 8], 8, Hkv, Hkv, 64, dtype, seed=seed)
+    g = torch.Generator().manual_seed(seed)
+    d["q"].zero_()
+    d["q"][..., 0] = d["q"][..., 1] = 1.0
+    for n in ("k_cache", "k_prefix"):
+        d[n].zero_()
+        d[n][..., 0] = 8.0 * level
+        d[n][..., 1] = torch.randint(-64, 64, d[n].shape[:-1], generator=g).to(d[n].dtype) / 8
+    d["v_prefix"][0, :keys // 2] = 1.0
+    d["v_prefix"][0, keys // 2:] = -1.0
+    return d
+
+
+@pytest.mark.parametrize("rows", [64, 256])
+def test_shared_partials_of_high_scores(rows):
+    # scores near 30208, their log-sum-exp in fp32 would be off by 2^-10: as a
+    # weight between partials that is 2^-10 of what they differ by, 2 A.  Here
+    # the weights are off by the exponents' rounding alone.  A segment adds at most
+    # 40 tiles, each key's weight through 4 sums a tile (half of them behind it) and
+    # then the merge's 64 candidates, 2^-24 each, and a weight is off by 2^-22:
+    # under 2^-16 A in all
+    d = high_scores(rows, 30208.0, "bf16", 35)
+    ro, rl, A = reference(d, 1 / 8)
+    out, lse = call(d, out_dtype=out_type("hilo"))
+    err = np.abs(out.cpu().numpy() - ro)
+    assert np.all(err <= 2.0 ** -16 * A), (err / A).max()
+    # lse passes five roundings of its own size (maximum, its sum with the
+    # logarithm, log2 e twice, the scale)
+    assert np.all(np.abs(lse.cpu().numpy() - rl) <= 5 * 2.0 ** -24 * np.abs(rl))
+    out, lse = call(d, out_dtype=out_type("bf16"), **roomy(d))
+    err = np.abs(out.double().cpu().numpy() - ro) - 2.0 ** -8 * np.abs(ro)
+    assert np.all(err <= 2.0 ** -15 * A), (err / A).max()
+
+
+@pytest.mark.parametrize("level", [0.0, 300.0, 30208.0])
+def test_shared_f32_is_float64_until_its_outputs(level):
+    # (the scale 1 / 8 is exact in float32) sums of 10^4 keys in float64, 2^-36 A; 64
+    # additions to each score, 2^-53 of it each, here and in the reference, and
+    # that twice, in the weights and in their sum: 2^-45 of the level; then one
+    # rounding of the output
+    d = high_scores(16, level, "f32", 36, keys=9000, Hkv=2)
+    import torch
+    g = torch.Generator().manual_seed(36)
+    d["q"][..., 2:] = torch.randn(d["q"][..., 2:].shape, generator=g)
+    for n in ("k_cache", "k_prefix"):
+        d[n][..., 2:] = torch.randn(d[n][..., 2:].shape, generator=g) / 4
+    ro, rl, A = reference(d, 1 / 8)
+    out, lse = call(d)
+    err = np.abs(out.cpu().numpy() - ro) - 2.0 ** -24 * np.abs(ro)
+    off = 2.0 ** -36 + 2.0 ** -45 * level
+    assert np.all(err <= off * A), (err / A).max()
+    assert np.all(np.abs(lse.cpu().numpy() - rl) <= 2.0 ** -24 * np.abs(rl) + off)
