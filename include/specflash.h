@@ -662,8 +662,9 @@ int sd_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_strid
  * alignment; 1 <= G <= B <= 2^16; Hq <= 2^16; B k Hq < 2^31; fewer than 2^27
  * tiles of 32 keys and 16 to 256 rows over all prefixes and sequences at
  * capacity; else SD_ERR_UNSUPPORTED (the workspace size is then 0).  A key
- * that is not finite reaches the rows that see it; a value that is not finite
- * may with SD_BF16 reach every row of its sequence.
+ * that is not finite reaches the rows that see it; so does a value with SD_F32 (an
+ * infinite one as itself), while with SD_BF16 it may reach every row of its
+ * sequence, as NaN.
  * ---------------------------------------------------------------------- */
 size_t sd_verify_shared_workspace_size(int B, int k, int Hq, int Hkv, int D, int G,
                                        int prefix_capacity, int capacity, int dtype);

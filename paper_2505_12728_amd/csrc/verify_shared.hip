@@ -839,7 +839,7 @@ __global__ __launch_bounds__(256) void shared_stream_f32(SharedArgs a, int G) {
     m = top;
     __syncthreads();
 #pragma unroll
-    for (int e = 0; e < PER; ++e) o[e] *= keep;
+    for (int e = 0; e < PER; ++e) o[e] = keep != 0.0 ? o[e] * keep : 0.0;
 #pragma unroll 8
     for (int t = 0; t < TK; ++t) {
       const double p = ps[r][t];
@@ -879,6 +879,9 @@ template <int ROWS, int TK, int D, bool SPLIT>
 __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G, int per, int wgs_seq) {
   constexpr int CH = D / 64, ROUND = 8;
   using F = PartT<ROWS>;
+  // infinite values stay infinite: a zero weight (a round's spare places, too) adds
+  // nothing.  On the matrix cores they are NaN already
+  constexpr bool kExact = ROWS == kRowsF32;
   __shared__ F part[4][2 + D];                // SPLIT: each wave's max, sum and channels
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int b = blockIdx.x / wgs_seq;
@@ -967,13 +970,13 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G, int per
       const F keep = weight_of(mx - nm);       // (0 from -inf)
       wsum *= keep;
 #pragma unroll
-      for (int e = 0; e < CH; ++e) acc[e] *= keep;
+      for (int e = 0; e < CH; ++e) acc[e] = kExact && keep == 0 ? 0 : acc[e] * keep;
 #pragma unroll
       for (int i = 0; i < ROUND; ++i) {
         const F wl = weight_of(ms[i] - nm) * ls[i];
         wsum += wl;
 #pragma unroll
-        for (int e = 0; e < CH; ++e) acc[e] = fma(wl, po[i][e], acc[e]);
+        for (int e = 0; e < CH; ++e) acc[e] = fma(wl, kExact && wl == 0 ? 0 : po[i][e], acc[e]);
       }
       mx = nm;
     }
@@ -996,7 +999,8 @@ __global__ __launch_bounds__(256) void shared_merge(SharedArgs a, int G, int per
         const F f = part[v][0] == nm ? 1 : weight_of(part[v][0] - nm);   // (-inf too)
         wsum = fma(f, part[v][1], wsum);
 #pragma unroll
-        for (int e = 0; e < CH; ++e) acc[e] = fma(f, part[v][2 + lane * CH + e], acc[e]);
+        for (int e = 0; e < CH; ++e)
+          acc[e] = fma(f, kExact && f == 0 ? 0 : part[v][2 + lane * CH + e], acc[e]);
       }
       mx = nm;
     }

@@ -162,3 +162,25 @@ def test_shared_f32_is_float64_until_its_outputs(level):
     off = 2.0 ** -36 + 2.0 ** -45 * level
     assert np.all(err <= off * A), (err / A).max()
     assert np.all(np.abs(lse.cpu().numpy() - rl) <= 2.0 ** -24 * np.abs(rl) + off)
+
+
+# ------------------------------------------------------ infinite values
+
+@pytest.mark.parametrize("keys", [200, 9000])
+def test_shared_f32_infinite_values_stay_infinite(keys):
+    # a value of +inf that a row sees makes that channel +inf, not NaN, and no
+    # other channel or row knows of it
+    d = inputs([9, 64, 70, 131], [keys], [4], 5, 4, 2, 128, "f32", seed=37)
+    d["v_prefix"][0, keys - 1, 1, 7] = math.inf          # every row of heads 2 and 3
+    for b, n in enumerate((9, 64, 70, 131)):
+        d["v_cache"][b, n - 1, 0, 3] = -math.inf          # the last block row of heads 0 and 1
+    with np.errstate(invalid="ignore"):
+        ref = reference(d, 1 / math.sqrt(128))
+    assert not np.isnan(ref[0]).any()
+    out, lse = call(d)
+    out = out.cpu().numpy()
+    bad = np.isinf(ref[0])
+    assert bad[:, :, 2:, 7].all() and bad[:, 4, :2, 3].all() and bad.sum() == 4 * 5 * 2 + 4 * 2
+    assert np.array_equal(out[bad], ref[0][bad].astype(np.float32))
+    assert np.all(np.abs(out - ref[0])[~bad] <= 2.0 ** -19 * ref[2][~bad])
+    assert np.all(np.abs(lse.cpu().numpy() - ref[1]) <= 1e-5)
