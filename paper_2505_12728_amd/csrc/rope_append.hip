@@ -10,9 +10,12 @@
 // -ang; the map being orthogonal, it is also the gradient.
 //
 // Angles are formed in float64 as turns, pos * f_i / (2 pi), and reduced
-// there (fp32 would leave 0.008 rad at position 10^5); only the reduced
-// fraction is rounded to fp32, for sincospi.  Products are fp32 and each
-// output is rounded once.
+// there (fp32 would leave 0.008 rad at position 10^5).  For fp32 outputs sine and
+// cosine are taken there too and rounded once: fp32 functions of the rounded
+// fraction are off by up to 1.5e-7 and save nothing from 16 heads on (20736 rows of
+// 16 heads of 80: 36 us with either; 65536 rows of a single head of 128: 27 us, 25
+// with those).  bf16 outputs, whose rounding is 2^16 times theirs, take the fp32
+// functions.  Products are fp32 and each output is rounded once.
 //
 // Bound by HBM: every element is read once and written once, 3 operations
 // between.  One wave takes one token at a time (or a share of its heads while
@@ -194,7 +197,14 @@ __global__ __launch_bounds__(kWavesWg * 64) void rope_rows(RopeArgs a) {
         double turn = (double)q * f[k];
         turn -= rint(turn);
         float sn, cs;
-        sincospif((float)(2.0 * turn), &sn, &cs);
+        if constexpr (sizeof(TD) == 4) {
+          double s64, c64;
+          sincospi(2.0 * turn, &s64, &c64);
+          sn = (float)s64;
+          cs = (float)c64;
+        } else {
+          sincospif((float)(2.0 * turn), &sn, &cs);
+        }
         table[w][i] = make_float2(cs, a.inverse ? -sn : sn);
       }
     }
