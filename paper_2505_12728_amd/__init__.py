@@ -862,6 +862,8 @@ def sd_rope(x, pos, theta, sections=None, per_axis=False, inverse=False, out=Non
     shape, xs = _rows(x, "x")
     T, H, D = shape
     dt = _dtype_code(x)
+    if pos is None:
+        raise ValueError(f"pos must be [axes, {T}] or [{T}], got None")
     axes, secs = _axes(pos, sections, T)
     if out is None:
         ys = H * D

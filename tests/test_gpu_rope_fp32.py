@@ -35,3 +35,10 @@ def test_fp32_turns_are_rounded_once(far, T, inverse, append):
     ref = oracle.rope_axes(x.numpy(), pos.numpy(), secs, 1e6, inverse=inverse)
     err = np.abs(y.cpu().numpy() - ref) - 2.0 ** -24 * np.abs(ref)
     assert np.all(err <= 20 * 2.0 ** -53 * far + 2.0 ** -50), err.max()
+
+
+def test_rope_needs_positions():
+    import torch
+    import paper_2505_12728_amd as sd
+    with pytest.raises(ValueError, match="pos"):
+        sd.sd_rope(torch.zeros(3, 2, 64, device="cuda"), None, 1e4)
