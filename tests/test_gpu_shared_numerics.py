@@ -184,3 +184,44 @@ def test_shared_f32_infinite_values_stay_infinite(keys):
     assert np.array_equal(out[bad], ref[0][bad].astype(np.float32))
     assert np.all(np.abs(out[~bad] - ref[0][~bad]) <= 2.0 ** -19 * ref[2][~bad])
     assert np.all(np.abs(lse.cpu().numpy() - ref[1]) <= 1e-5)
+
+
+# -------------------------------------- forms of the kernels that no other test runs
+
+@pytest.mark.parametrize("kind", ["hilo", "bf16", "f32"])
+@pytest.mark.parametrize("B,k,Hq,Hkv", [(60, 7, 45, 5), (90, 7, 45, 5), (50, 7, 56, 8)])
+def test_shared_merge_waves_of_several_rows(kind, B, k, Hq, Hkv):
+    # 16384 rows and more: a merge wave takes two or three of them, of 315 or 392
+    # rows a sequence, so that last shares are short and some waves have none
+    lens = [k + (11 * b) % 90 for b in range(B)]
+    sizes = [B // 2, 0, B // 3]
+    d = inputs(lens, [150, 9, 65], sizes, k, Hq, Hkv, 64, "f32" if kind == "f32" else "bf16", seed=38, lead=1,
+               left=B - sum(sizes) - 1)
+    out, lse = call(d, out_dtype=out_type(kind))
+    check(d, out, lse, reference(d, 1 / 8), kind)
+
+
+@pytest.mark.parametrize("kind", ["hilo", "bf16", "f32"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_shared_rows_that_see_a_nonfinite_key(kind, bad):
+    # the last key of a sequence, in one channel: the last block row alone.  Its
+    # scores are NaN or +inf, which leave no softmax, or -inf, a key of no weight
+    d = inputs([9, 64, 70, 131], [200], [4], 5, 4, 2, 128, "f32" if kind == "f32" else "bf16", seed=39)
+    for b, n in enumerate((9, 64, 70, 131)):
+        d["k_cache"][b, n - 1, :, 11] = bad
+    d["q"][:, :, 0, 11], d["q"][:, :, 1:, 11] = 1.0, -1.0
+    with np.errstate(invalid="ignore"):
+        ro, rl, A = reference(d, 1 / math.sqrt(128))
+    none = np.isnan(rl)
+    assert none[:, 4].sum() == {math.inf: 4, -math.inf: 12}.get(bad, 16) and not none[:, :4].any()
+    out, lse = call(d, out_dtype=out_type(kind))
+    assert np.array_equal(np.isnan(out.float().cpu().numpy()).all(-1), none)
+    assert np.array_equal(np.isnan(lse.cpu().numpy()), none)
+    out[torch_mask(none)], lse[torch_mask(none)] = 0.0, 0.0
+    ro[none], rl[none], A[none] = 0.0, 0.0, 0.0
+    check(d, out, lse, (ro, rl, A), kind)
+
+
+def torch_mask(x):
+    import torch
+    return torch.from_numpy(x).cuda()
