@@ -683,9 +683,9 @@ __global__ __launch_bounds__(512, 2) void shared_stream_bf16(SharedArgs a, int G
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb) top = seen_max(ex[kb][rb], t_first + kb * 16 + 4 * G4, rb, top);
         top = wave_max_across_groups(top);
-        // no finite score here (none that the row sees, or -inf alone): l stays 0,
-        // and the first finite one raises m from the lowest value
-        m[rb] = top == -FLT_MAX ? -FLT_MAX : top * sl2;
+        // no finite score here (none that the row sees, -inf alone, or below the
+        // range once scaled): l stays 0, and the first that is one raises m
+        m[rb] = fmaxf(top * sl2, -FLT_MAX);
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb) exponents(ex[kb][rb], rb);
         l[rb] = 0.f;

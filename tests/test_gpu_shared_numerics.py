@@ -93,6 +93,24 @@ def test_shared_tiles_of_minus_infinity(how, rows, level):
         check(d, out, lse, ref, kind, 300 / 8)
 
 
+@pytest.mark.parametrize("rows", [64, 256])
+@pytest.mark.parametrize("scale", [64.0, -64.0])
+def test_shared_tiles_below_the_range_once_scaled(rows, scale):
+    # every other tile's products are finite, -3e37, and pass fp32's range with the
+    # scale alone: weight 0 as well
+    d = long_groups(rows, seed=40)
+    d["q"] = d["q"] / 512
+    d["q"][..., 0] = 1e19 * np.sign(scale)
+    d["q"][..., 1] = np.sign(scale)
+    for n in ("k_cache", "k_prefix"):
+        d[n][..., 1] = -300 / 64
+    every_other_tile(d, 0, -3e18)
+    ref = reference(d, scale)
+    for kind in ("hilo", "bf16"):
+        out, lse = call(d, scale=scale, out_dtype=out_type(kind), **(roomy(d) if kind == "bf16" else {}))
+        check(d, out, lse, ref, kind, 300 / 8)
+
+
 @pytest.mark.parametrize("kind", ["hilo", "bf16", "f32"])
 def test_shared_only_minus_infinity_is_no_key(kind):
     # rows all of whose scores are -inf see nothing: out 0 and lse -inf
