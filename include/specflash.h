@@ -563,8 +563,9 @@ int sd_semi_ar_draft(const void* u0, const void* fc_w, const float* fc_b, const 
  *             element of y is an element of x
  *   pos       [num_axes, T] int32, any values
  *   sections  [num_axes] HOST array, or NULL for one axis of D / 2 pairs
- * Angles are reduced in float64, products are float32, y is rounded once to
- * dtype (the one output here that is not float32: it feeds the attention).
+ * Angles are reduced in float64 (with SD_F32 their sines and cosines are taken
+ * there too), products are float32, y is rounded once to dtype (the one output
+ * here that is not float32: it feeds the attention).
  * Requirements: T >= 0 (0 launches nothing), H >= 1, 1 <= num_axes <= 4,
  * sections >= 1 with a sum of at most D / 2, D <= 256, T <= 2^30, H <= 2^20,
  * strides >= H D and <= 2^32, theta > 0 and finite.  Any alignment that dtype
@@ -601,7 +602,9 @@ int sd_rope(const void* x, int64_t x_stride, const int32_t* pos, void* y, int64_
  *   kv_len    [B] int32: cache length after the append
  *   page_table [B, max_pages] int32, or NULL
  *   pos       [num_axes, T] int32 rotary positions, or NULL: the cache
- *             position on every axis
+ *             position on every axis.  Behind a shared prefix (sd_verify_shared)
+ *             a sequence's own cache begins at 0 again: give pos there, for text
+ *             the prefix's length plus the cache position
  *   num_axes, sections, theta, freq  as for sd_rope; num_axes = 0 turns
  *             nothing (keys that carry their positions already)
  * A row whose cache position lies outside 0 .. capacity - 1, or whose page id
@@ -622,8 +625,9 @@ int sd_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_strid
 
 /* ------------------------------------------------------------------------
  * Verification attention of sequences that share long prefixes (several
- * questions about one video, several answers to one prompt): a prefix is read
- * and attended once for all sequences of its group.
+ * questions about one video, several answers to one prompt): a prefix is
+ * attended once by all rows of its group, and read once for each tile of 128 or
+ * 256 such rows of a KV head (16 with SD_F32), not once per sequence.
  *
  * The B sequences lie in G groups: group i holds the sequences group_start[i]
  * .. group_start[i + 1] - 1 (NULL: B / G each).  Every row of a group sees the
@@ -657,7 +661,10 @@ int sd_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_strid
  * SD_BF16 with out_dtype SD_F32 feeds the probabilities to the second product
  * as sums of three bf16 (all of their float32 bits); with out_dtype SD_BF16 as
  * sums of two (16 bits, below the rounding of out itself).
- * SD_F32 runs in float64 and gives SD_F32.
+ * SD_F32 runs in float64, partial results included, and gives SD_F32.
+ * The rows per tile follow the capacities, since lengths are known on the device
+ * alone: a table or cache much wider than its prefixes costs a few us (the tiles
+ * suit long ones).
  * Requirements: those of sd_verify_attention for k, Hq, Hkv, D, scale and
  * alignment; 1 <= G <= B <= 2^16; Hq <= 2^16; B k Hq < 2^31; fewer than 2^27
  * tiles of 32 keys and 16 to 256 rows over all prefixes and sequences at

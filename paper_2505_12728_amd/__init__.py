@@ -886,8 +886,9 @@ def sd_kv_append(q, k, v, k_cache, v_cache, kv_len, theta, pos=None, sections=No
     [P, Hkv, 16, D] with page_table [B, max_pages] int32; kv_len [B] int32, the
     lengths after the append.  row_start [B + 1] int32 names each sequence's
     rows (None: T / B rows each, in order).  Keys and queries are rotated at pos
-    [T] or [axes, T] int32 (None: their cache position; theta None: not at
-    all), see sd_rope.  fp32 rows may go into a bf16 cache.  The caches are
+    [T] or [axes, T] int32 (None: their cache position, which behind a shared
+    prefix starts at 0 again: give pos there; theta None: not at all), see
+    sd_rope.  fp32 rows may go into a bf16 cache.  The caches are
     written in place.  Returns the rotated queries [T, Hq, D] in the cache's
     dtype (None without q)."""
     int32 = _torch().int32
@@ -979,6 +980,10 @@ def sd_verify_shared(q, k_cache, v_cache, kv_len, prefix_len, k_prefix=None, v_p
                      group_start=None, page_table=None, num_pages=None, scale=None, out_dtype=None, out=None, lse=True,
                      workspace=None, stream=None):
     """Verification attention of sequences in groups that share a prefix.
+
+    Own keys carry the positions that they were appended with: behind a prefix
+    that is pos = prefix length + place in the own cache (text), which
+    sd_kv_append takes as its pos.
 
     q [B, k, Hq, D]; own caches [B, Lmax, Hkv, D], or page pools [P, Hkv, 16,
     D] with page_table [B, max_pages]; kv_len [B] counts own keys, the block

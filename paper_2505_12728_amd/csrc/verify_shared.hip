@@ -7,7 +7,9 @@
 // (m, l, O) over disjoint key sets combine exactly, so that a prefix is
 // attended once by all rows of its group (S k g rows of a KV head: S
 // sequences, k block positions, g query heads) and its keys and values are
-// read from HBM once, not once per sequence.
+// read once for each tile of those rows (128 or 256 of them, 16 for fp32), not
+// once per sequence.  Tiles of one prefix run at different times on different
+// XCDs: what they read again comes from the memory-side cache at best.
 //
 // Bound: 4 D operations per (row, key) against 4 D bytes per key and KV head
 // (bf16), so HBM up to about 300 rows per KV head and the matrix cores beyond.
@@ -49,13 +51,14 @@ constexpr int kTileF32 = 32, kTile = 64;   // keys per tile (fp32, bf16)
 constexpr int kRowsF32 = 16;               // rows per work-group (fp32)
 // Places that the list gives to a tile and to the start of a pair (its queries'
 // latency, the partial of the one before), so that equal ranges take equal times.
-// On the matrix cores, in thirds of a tile whose rows are all there (about 2.2 us):
-// a tile with half of them or fewer takes two (1.4 us with fp32 outputs, 1.3 in
-// tiles of 256 rows), a start six, which one-tile pairs need, whose latencies
-// nothing hides (3.9 us; pairs of 11 tiles 2.2).  Whole tiles for all and two for a
-// start: own caches of 24 rows and 700 keys took 39 us where the prefixes' work-groups
-// took 60 (the call 73.5 us, 70.5 so); three thirds for a start: 1024 rows with 64 own
-// keys 378 us against 330.
+// On the matrix cores, in thirds of a tile whose rows are all there (measured with P
+// in one term for bf16 outputs, when such a tile took about 2.2 us): a tile with
+// half of them or fewer takes two (1.4 us with fp32 outputs, 1.3 in tiles of 256
+// rows), a start six, which one-tile pairs need, whose latencies nothing hides (3.9
+// us; pairs of 11 tiles 2.2).  Whole tiles for all and two for a start: own caches of
+// 24 rows and 700 keys took 39 us where the prefixes' work-groups took 60 (the call
+// 73.5 us, 70.5 so); three thirds for a start: 1024 rows with 64 own keys 378 us
+// against 330.
 constexpr int kWhole = 3, kStartPlaces = 6;
 constexpr int start_places(int rows_wg) { return rows_wg == kRowsF32 ? 0 : kStartPlaces; }
 constexpr int most_places(int rows_wg) { return rows_wg == kRowsF32 ? 1 : kWhole; }
@@ -298,11 +301,12 @@ __device__ __forceinline__ int out_row(const SharedArgs& a, int first, int hk, i
 // runs in groups of four LDS fragments: a group's reads are issued one group
 // ahead and waited for by count.  K and V have rings of four slots: a tile's copy
 // has two steps to land.
-//   64 rows over 65500 keys of 8 heads of 128 (268 MB): 50 us, 5.4 TB/s, HBM.
-//   1024 rows there, bf16 out (275 GFLOP in the formula, 413 in two terms):
-// the call with its merge 369 us, 1120 TFLOP/s of products, where one of 8192^3
-// reaches 1346.  No LDS conflicts.  A step's 96 matrix instructions take 1536
-// cycles of a wave.
+//   64 rows over 65500 keys of 8 heads of 128 (268 MB): 47 us, 5.7 TB/s, HBM.
+//   1024 rows there, bf16 out (275 GFLOP in the formula, 413 in two terms): 350
+// us, 1180 TFLOP/s of products, where one of 8192^3 reaches 1346.  Matrix cores
+// busy 54%, no LDS conflicts.  A step's 96 matrix instructions take 1536 cycles of
+// a wave, its 230 vector ones (32 of them exponentials) about 1300; the two waves
+// of a SIMD overlap them little.
 template <int V>
 struct Const {
   static constexpr int value = V;
